@@ -67,7 +67,10 @@ typedef enum { CP_BF16 = 0, CP_FP32 = 1 } cp_dtype;
 typedef enum {
   CP_WS_PARTIAL = 0, /* cp_attn_partial  */
   CP_WS_DECODE = 1,  /* cp_attn_decode   */
-  CP_WS_MERGE = 2    /* cp_attn_merge (needs none; returns 0) */
+  CP_WS_MERGE = 2,   /* cp_attn_merge (needs none; returns 0) */
+  CP_WS_TREE = 3,    /* cp_tree_attn */
+  CP_WS_WEIGHT = 4,  /* cp_kv_attn_weight */
+  CP_WS_EVICT = 5    /* cp_kv_evict */
 } cp_ws_kind;
 
 /*
@@ -507,6 +510,125 @@ int cp_kv_append(const cp_shape* shape, const void* k_new, const void* v_new,
                  const int32_t* pos_new, const int32_t* cu_seqlens_new, void* k_cache,
                  void* v_cache, int32_t* kv_pos_cache, const int32_t* cu_seqlens_kv,
                  int32_t* seq_used, int32_t* dropped, void* stream);
+
+/*
+ * Speculative decoding on a rank's cache. A draft model proposes, for every sequence b, a tree of
+ * n_b tokens, one node each; the model's queries of all nodes are answered in one call
+ * (cp_tree_attn), the path that the verification accepts goes into the cache (cp_tree_accept), the
+ * rest is dropped. Nodes of all trees are packed, cu_seqlens_q[b] .. cu_seqlens_q[b+1] being
+ * sequence b's, every node behind its parent. Node i's mask is `mask_words` 64-bit words, bit t % 64
+ * of word t / 64 for node t of its tree (by its index within the tree); a node that sees itself has
+ * its own bit set. Bits of nodes that the tree does not have are ignored, and nodes that the words
+ * have no bit for are seen by none.
+ */
+#define CP_TREE_MAX_WORDS 16
+
+/*
+ * Host arithmetic: the masks of trees given by their nodes' parents (index within the tree, -1: the
+ * node follows the cached tokens directly). A node sees its ancestors and itself.
+ *   cu_seqlens (host) int32 [batch+1], parents (host) int32 [cu_seqlens[batch]]
+ *   mask_out   (host) uint64 [cu_seqlens[batch], mask_words]
+ * CP_ERR_SHAPE: batch < 1, mask_words outside 1 .. CP_TREE_MAX_WORDS, boundaries that do not begin
+ * at 0 or fall, a tree of more than 64 * mask_words nodes, a parent that is not in front of its node.
+ */
+int cp_tree_mask(int32_t batch, const int32_t* cu_seqlens, const int32_t* parents,
+                 int32_t mask_words, uint64_t* mask_out);
+
+/*
+ * Attention of the drafted trees: O and LSE, as cp_attn_partial's, of every node over
+ *   - its sequence's cached tokens: slots [cu_seqlens_kv[b], + seq_used[b]) with kv_pos <= q_pos,
+ *   - the nodes of its own tree that its mask names.
+ *
+ *   shape->batch    sequences;  shape->total_q  nodes of all trees;  shape->total_kv  cache slots
+ *   q               (device) [total_q, n_q_heads, head_dim]
+ *   q_pos           (device) int32 [total_q]: position of the node's token (its depth counted from
+ *                   the sequence's length), for the cached tokens' mask
+ *   cu_seqlens_q    (device) int32 [batch+1]
+ *   k_new, v_new    (device) [total_q, n_kv_heads, head_dim], the nodes' own K and V; both NULL: the
+ *                   nodes see the cached tokens only (a rank of a ring that does not hold the trees;
+ *                   cp_attn_merge joins the ranks' results), and tree_mask is not read
+ *   tree_mask       (device) uint64 [total_q, mask_words], 1 <= mask_words <= CP_TREE_MAX_WORDS
+ *   k_cache ... cu_seqlens_kv, seq_used  the cache as described at cp_kv_append; seq_used may be
+ *                   NULL (every slot of a sequence's range is read)
+ *   out, lse        as cp_attn_partial; rows behind cu_seqlens_q[batch] are left as they were
+ *   workspace       cp_workspace_bytes(shape, CP_WS_TREE) bytes, 256-byte aligned
+ *
+ * bf16 and fp32, head_dim 64 and 128, any group of query heads. What a node does not see does not
+ * reach it, NaN and infinity in hidden K and V rows included. Scores, statistics and accumulators
+ * are fp32; with bf16 inputs the probabilities are rounded to bf16 where out is bf16, and keep 24 bits
+ * where it is fp32. Two launches. Boundaries and counts on the device that contradict the shape
+ * are cut to it: nothing outside the tensors is read or written.
+ */
+int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
+                 const int32_t* cu_seqlens_q, const void* k_new, const void* v_new,
+                 const uint64_t* tree_mask, int32_t mask_words, const void* k_cache,
+                 const void* v_cache, const int32_t* kv_pos_cache, const int32_t* cu_seqlens_kv,
+                 const int32_t* seq_used, void* out, float* lse, int32_t out_dtype, void* workspace,
+                 size_t workspace_bytes, void* stream);
+
+/*
+ * Appends the accepted paths to the cache: for every sequence b the K/V rows and positions of the
+ * nodes that the mask of node accepted[b] names, in the order of their indices, as cp_kv_append would.
+ *   shape->dtype, head_dim, n_kv_heads, batch, total_q (nodes), total_kv (slots) as in cp_kv_append
+ *   accepted  (device) int32 [batch]: the last accepted node, by its index within the tree; one
+ *             that the tree does not have, or a negative one, accepts nothing
+ *   dropped   (device) int32 or NULL: incremented by the number of rows that did not fit
+ *   other arguments as cp_tree_attn and cp_kv_append. One launch, no workspace.
+ */
+int cp_tree_accept(const cp_shape* shape, const void* k_new, const void* v_new,
+                   const int32_t* pos_new, const int32_t* cu_seqlens_new, const uint64_t* tree_mask,
+                   int32_t mask_words, const int32_t* accepted, void* k_cache, void* v_cache,
+                   int32_t* kv_pos_cache, const int32_t* cu_seqlens_kv, int32_t* seq_used,
+                   int32_t* dropped, void* stream);
+
+/*
+ * A cache of bounded size. Every slot carries the attention weight that it has received; what has
+ * received least is evicted.
+ *
+ * cp_kv_attn_weight: for every token in the cache, slot j of sequence b,
+ *   weight[j] <- decay * weight[j] + sum over the queries i of sequence b with kv_pos[j] <= q_pos[i],
+ *                and over all heads h, of exp(softmax_scale * q_ih . k_j - lse[i][h]).
+ * With the LSE of the finished attention (over all ranks, merged) the terms are its probabilities.
+ *   shape->total_q  queries (packed by sequence, cu_seqlens_q);  shape->total_kv  cache slots
+ *   lse       (device) fp32 [total_q, n_q_heads]; a query of LSE -inf weighs nothing
+ *   decay     >= 0, finite; 0: weight is overwritten without being read
+ *   weight    (device) fp32 [slots]; slots that hold no token are left as they were (new tokens come
+ *             to slots of weight 0 if the array was cleared with the cache: cp_kv_evict clears what it
+ *             frees)
+ *   workspace cp_workspace_bytes(shape, CP_WS_WEIGHT) bytes, 256-byte aligned; may be NULL if 0
+ * bf16 and fp32, head_dim 64 and 128, any group of query heads. fp32 arithmetic, sums in a fixed
+ * order. What a query does not see does not reach the sum. One launch, or two with a workspace.
+ */
+int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int32_t* q_pos,
+                      const int32_t* cu_seqlens_q, const float* lse, const void* k_cache,
+                      const int32_t* kv_pos_cache, const int32_t* cu_seqlens_kv,
+                      const int32_t* seq_used, float decay, float* weight, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/*
+ * Shrinks every sequence of a cache to its budget. Of the n = seq_used[b] tokens of sequence b
+ *   keep = min(n, room of the destination, max(budget[b], number of protected tokens))
+ * stay: the protected ones first (kv_pos < sinks, or kv_pos >= protect_from[b]; a padded token is
+ * never protected), then by weight, ties to the lowest slot; a NaN counts as the lowest weight.
+ * Kept tokens in slots 0 .. keep-1 of the sequence's range stay in their slot, and the i-th kept token
+ * behind them takes the i-th slot that became free among them. (The order of the slots means
+ * nothing to attention, which goes by kv_pos.) Slots behind the kept tokens get CP_POS_PAD_KV and
+ * weight 0; their K and V are left as they were.
+ *   shape     dtype, head_dim, n_kv_heads, batch, total_kv (slots) as in cp_kv_append
+ *   budget    (device) int32 [batch]; below 0 counts as 0
+ *   protect_from (device) int32 [batch] or NULL (no token is protected for being recent)
+ *   k_to ... seq_used_to, slots_to  another cache and its weights, of the same row shape and batch,
+ *             which receives the kept tokens (what it held is given up; the source is left as it was); or
+ *             all NULL and 0: in place. The two caches do not overlap.
+ *   workspace cp_workspace_bytes(shape, CP_WS_EVICT) bytes, 256-byte aligned
+ * Two launches. The result does not depend on the order in which anything runs.
+ */
+int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, int32_t* kv_pos_cache,
+                float* weight, const int32_t* cu_seqlens_kv, int32_t* seq_used,
+                const int32_t* budget, const int32_t* protect_from, int32_t sinks, void* k_to,
+                void* v_to, int32_t* kv_pos_to, float* weight_to, const int32_t* cu_seqlens_to,
+                int32_t* seq_used_to, int64_t slots_to, void* workspace, size_t workspace_bytes,
+                void* stream);
 
 /*
  * Host arithmetic. Rank that takes sequence `seq`'s token (its query, and its K/V in that

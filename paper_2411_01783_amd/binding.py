@@ -21,6 +21,8 @@ CALLS_PATH = os.path.join(_HERE, "_py_calls.so")
 
 CP_BF16, CP_FP32 = 0, 1
 CP_WS_PARTIAL, CP_WS_DECODE, CP_WS_MERGE = 0, 1, 2
+CP_WS_TREE, CP_WS_WEIGHT, CP_WS_EVICT = 3, 4, 5
+CP_TREE_MAX_WORDS = 16
 CP_POS_PAD_KV = 2**31 - 1
 CP_POS_PAD_Q = -1
 CP_MAX_PARTS = 64
@@ -32,6 +34,7 @@ EXPORTS = [
     "cp_attn_merge", "cp_ring_passkv", "cp_ring_passq", "cp_ring_passq_decode",
     "cp_ring_workspace_bytes", "cp_ring_message_bytes", "cp_ring_prefill", "cp_select_order", "cp_kv_cache_reset", "cp_kv_append",
     "cp_decode_owner", "cp_strerror",
+    "cp_tree_mask", "cp_tree_attn", "cp_tree_accept", "cp_kv_attn_weight", "cp_kv_evict",
     "cp_version",
 ]
 CP_STATIC_SCRATCH_BYTES = 8 << 20
@@ -140,6 +143,19 @@ def load() -> ctypes.CDLL:
     lib.cp_kv_append.argtypes = [ctypes.POINTER(cp_shape)] + [_vp] * 11
     lib.cp_decode_owner.restype = _i32
     lib.cp_decode_owner.argtypes = [_i32, _i32, _i32]
+    lib.cp_tree_mask.restype = ctypes.c_int
+    lib.cp_tree_mask.argtypes = [_i32, ctypes.POINTER(_i32), ctypes.POINTER(_i32), _i32, _vp]
+    lib.cp_tree_attn.restype = ctypes.c_int
+    lib.cp_tree_attn.argtypes = [ctypes.POINTER(cp_shape)] + [_vp] * 6 + [_i32] + [_vp] * 7 + \
+        [_i32, _vp, ctypes.c_size_t, _vp]
+    lib.cp_tree_accept.restype = ctypes.c_int
+    lib.cp_tree_accept.argtypes = [ctypes.POINTER(cp_shape)] + [_vp] * 5 + [_i32] + [_vp] * 8
+    lib.cp_kv_attn_weight.restype = ctypes.c_int
+    lib.cp_kv_attn_weight.argtypes = [ctypes.POINTER(cp_shape)] + [_vp] * 8 + [_f32] + [_vp] * 2 + \
+        [ctypes.c_size_t, _vp]
+    lib.cp_kv_evict.restype = ctypes.c_int
+    lib.cp_kv_evict.argtypes = [ctypes.POINTER(cp_shape)] + [_vp] * 8 + [_i32] + [_vp] * 6 + \
+        [_i64, _vp, ctypes.c_size_t, _vp]
     spec = importlib.util.spec_from_file_location("_py_calls", CALLS_PATH)
     native = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(native)
@@ -147,6 +163,8 @@ def load() -> ctypes.CDLL:
         "cp_workspace_bytes", "cp_attn_partial", "cp_attn_decode", "cp_attn_decode_static",
         "cp_attn_merge", "cp_kv_append", "cp_ring_passkv", "cp_ring_passq",
         "cp_ring_passq_decode")])
+    native.connect_cache(*[ctypes.cast(getattr(lib, name), _vp).value for name in (
+        "cp_tree_attn", "cp_tree_accept", "cp_kv_attn_weight", "cp_kv_evict")])
     _lib, _native = lib, native
     return lib
 
@@ -387,6 +405,87 @@ def cp_kv_append(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor,
                                      cache.slots, cache.batch, _raw(stream))
     if r:
         raise CpError(r, "cp_kv_append")
+
+
+def cp_tree_mask(parents, cu_seqlens, words: Optional[int] = None) -> np.ndarray:
+    """Mask words (int64 [nodes, words]) of trees given by their nodes' parents (-1: the node follows
+    the cached tokens); the trees' nodes are packed, [cu[b], cu[b+1]). Host only."""
+    parents = np.ascontiguousarray(np.asarray(parents, dtype=np.int32))
+    cu = np.ascontiguousarray(np.asarray(cu_seqlens, dtype=np.int32))
+    if parents.ndim != 1 or cu.ndim != 1 or cu.size < 2 or parents.size != cu[-1]:
+        raise ValueError("parents and cu_seqlens do not match")
+    if words is None:
+        words = max(1, (int(np.diff(cu).max()) + 63) // 64)
+    mask = np.zeros((parents.size, words), dtype=np.int64)
+    at = ctypes.POINTER(_i32)
+    _check(load().cp_tree_mask(cu.size - 1, cu.ctypes.data_as(at), parents.ctypes.data_as(at), words,
+                               mask.ctypes.data), "cp_tree_mask")
+    return mask
+
+
+def cp_tree_attn(cache: KVCache, q: torch.Tensor, q_pos: torch.Tensor,
+                 k_new: Optional[torch.Tensor], v_new: Optional[torch.Tensor],
+                 cu_seqlens_q: torch.Tensor, tree_mask: Optional[torch.Tensor],
+                 out_dtype: Optional[torch.dtype] = None, softmax_scale: float = 0.0, out=None,
+                 lse=None, workspace=None, stream=None):
+    """(O, LSE) of the drafted nodes q [nodes, N_H, d] over their sequence's cached tokens
+    (kv_pos <= q_pos) and the nodes of their own tree that tree_mask names. k_new = v_new =
+    tree_mask = None: over the cached tokens only (a rank that does not hold the trees)."""
+    args = (q, q_pos, cu_seqlens_q, k_new, v_new, tree_mask, cache.k, cache.v, cache.kv_pos, cache.cu,
+            cache.used, out_dtype, softmax_scale, out, lse, workspace, _raw(stream))
+    call = (_native or _calls()).tree_attn
+    other = None
+    if stream is not None and (out is None or lse is None or workspace is None):
+        other = _elsewhere(stream, q)
+    r = call(*args) if other is None else _allocated_there(other, q, lambda: call(*args), out, lse)
+    if type(r) is int:
+        raise CpError(r, "cp_tree_attn")
+    return r
+
+
+def cp_tree_accept(cache: KVCache, k_new: torch.Tensor, v_new: torch.Tensor, pos_new: torch.Tensor,
+                   cu_seqlens_new: torch.Tensor, tree_mask: torch.Tensor, accepted: torch.Tensor,
+                   stream=None) -> None:
+    """Append the rows of the nodes that the mask of node accepted[b] (an index within the tree; -1:
+    none) names to sequence b of the cache."""
+    r = (_native or _calls()).tree_accept(k_new, v_new, pos_new, cu_seqlens_new, tree_mask, accepted,
+                                          cache.k, cache.v, cache.kv_pos, cache.cu, cache.used,
+                                          cache.dropped, _raw(stream))
+    if r:
+        raise CpError(r, "cp_tree_accept")
+
+
+def cp_kv_attn_weight(cache: KVCache, q: torch.Tensor, q_pos: torch.Tensor, lse: torch.Tensor,
+                      weight: torch.Tensor, cu_seqlens_q: torch.Tensor, decay: float = 1.0,
+                      softmax_scale: float = 0.0, workspace=None, stream=None) -> torch.Tensor:
+    """weight [slots] <- decay * weight + the attention weight of every cached token under the queries
+    q [queries, N_H, d] of its sequence, whose finished attention has the log-sum-exp `lse`."""
+    args = (q, q_pos, cu_seqlens_q, lse, weight, cache.k, cache.v, cache.kv_pos, cache.cu, cache.used,
+            decay, softmax_scale, workspace, _raw(stream))
+    call = (_native or _calls()).kv_weight
+    other = None if stream is None or workspace is not None else _elsewhere(stream, q)
+    r = call(*args) if other is None else _allocated_there(other, q, lambda: call(*args))
+    if r:
+        raise CpError(r, "cp_kv_attn_weight")
+    return weight
+
+
+def cp_kv_evict(cache: KVCache, weight: torch.Tensor, budget: torch.Tensor,
+                protect_from: Optional[torch.Tensor] = None, sinks: int = 0,
+                into: Optional[KVCache] = None, into_weight: Optional[torch.Tensor] = None,
+                workspace=None, stream=None) -> None:
+    """Shrink every sequence of the cache to budget[b] tokens, those of the largest weight; tokens at
+    positions below `sinks` or from protect_from[b] on go last. In place, or into another cache."""
+    if (into is None) != (into_weight is None):
+        raise ValueError("into and into_weight come together")
+    to = (None,) * 6 if into is None else (into.k, into.v, into.kv_pos, into.cu, into.used, into_weight)
+    args = (cache.k, cache.v, cache.kv_pos, cache.cu, cache.used, weight, budget, protect_from, sinks) \
+        + to + (workspace, _raw(stream))
+    call = (_native or _calls()).kv_evict
+    other = None if stream is None or workspace is not None else _elsewhere(stream, cache.k)
+    r = call(*args) if other is None else _allocated_there(other, cache.k, lambda: call(*args))
+    if r:
+        raise CpError(r, "cp_kv_evict")
 
 
 def cp_decode_owner(seq: int, decode_iter: int, n_ranks: int) -> int:

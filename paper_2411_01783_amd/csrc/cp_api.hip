@@ -9,10 +9,7 @@
 
 using namespace cp;
 
-namespace {
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
+namespace cp {
 
 int check_shape(const cp_shape* s) {
   if (s == nullptr) return CP_ERR_NULL;
@@ -26,6 +23,24 @@ int check_shape(const cp_shape* s) {
   if (!(s->softmax_scale == s->softmax_scale) || isinf(s->softmax_scale)) return CP_ERR_SHAPE;
   return CP_OK;
 }
+
+int check_cache_shape(const cp_shape* s) {
+  if (s == nullptr) return CP_ERR_NULL;
+  if (s->dtype != CP_BF16 && s->dtype != CP_FP32) return CP_ERR_UNSUPPORTED;
+  if (s->head_dim < 8 || s->head_dim > 256 || s->head_dim % 8 != 0) return CP_ERR_UNSUPPORTED;
+  if (s->n_kv_heads < 1 || s->batch < 1 || s->total_q < 0 || s->total_kv < 0) return CP_ERR_SHAPE;
+  if (s->total_q > INT32_MAX || s->total_kv > INT32_MAX) return CP_ERR_SHAPE;
+  // 16-byte chunks of a row are counted in 31 bits
+  if ((int64_t)s->n_kv_heads * s->head_dim > INT32_MAX / 4) return CP_ERR_SHAPE;
+  return CP_OK;
+}
+
+}  // namespace cp
+
+namespace {
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
 
 inline float resolve_scale(float scale, int head_dim) {
   return scale > 0.f ? scale : 1.0f / sqrtf((float)head_dim);
@@ -131,6 +146,8 @@ int cp_shard_positions(int64_t total, int64_t offset, int32_t n_ranks, int32_t r
 }
 
 size_t cp_workspace_bytes(const cp_shape* shape, int32_t kind) {
+  if (kind == CP_WS_EVICT)   // (head_dim as the cache's, not attention's)
+    return check_cache_shape(shape) == CP_OK ? evict_workspace_bytes(*shape) : 0;
   if (check_shape(shape) != CP_OK) return 0;
   switch (kind) {
     case CP_WS_PARTIAL:
@@ -141,6 +158,10 @@ size_t cp_workspace_bytes(const cp_shape* shape, int32_t kind) {
                   : 0);
     case CP_WS_DECODE:
       return decode_workspace_bytes(*shape);
+    case CP_WS_TREE:
+      return tree_workspace_bytes(*shape);
+    case CP_WS_WEIGHT:
+      return weight_workspace_bytes(*shape);
     default:
       return 0;
   }

@@ -57,6 +57,15 @@ __device__ __forceinline__ int touch_arguments() {
 // ---- launchers (each returns a cp_status; enqueue on `stream` only) ----
 
 // fp32 vector kernel: any supported dtype / head_dim, packed batches.
+// Argument checks on a shape: of an attention call, of a call on the KV cache alone (cp_api.hip).
+int check_shape(const cp_shape* s);
+int check_cache_shape(const cp_shape* s);
+
+// Workspaces of cp_tree_attn, cp_kv_attn_weight and cp_kv_evict.
+size_t tree_workspace_bytes(const cp_shape& s);
+size_t weight_workspace_bytes(const cp_shape& s);
+size_t evict_workspace_bytes(const cp_shape& s);
+
 int launch_partial_generic(const cp_shape& s, float scale, const void* q, const void* k,
                            const void* v, const int32_t* q_pos, const int32_t* kv_pos,
                            const int32_t* cu_q, const int32_t* cu_kv, void* out, float* lse,

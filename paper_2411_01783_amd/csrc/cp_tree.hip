@@ -1,0 +1,934 @@
+// Attention of trees of drafted tokens over the persistent KV cache (speculative decoding on a
+// rank's share of it), and the commit of the accepted paths.
+//
+// Sequence b has n_b drafted nodes. Node i sees cache slot j < used_b iff kv_pos[j] <= q_pos[i],
+// and node t of its own tree iff bit t of its mask is set. With s_j = scale q.k_j over what it sees,
+//   O = sum_j e^(s_j - m) v_j / sum_j e^(s_j - m),   LSE = m + log sum_j e^(s_j - m),
+// in one pass over the keys with a running maximum m and sum (online softmax).
+//
+// The n_b nodes times the `group` query heads of a KV head are the rows of one product against that
+// head's keys; rows are cut into row blocks and keys into sub-tiles of 32, first the cached ones,
+// then the tree's own. S^T = K Q^T and O^T += V^T P^T run on 32x32 MFMAs with the keys (channels) on
+// the M side and the rows on the N side, which keeps a row's statistics in one lane pair and
+// feeds P to the second product from the registers the first one left it in.
+//
+// All (KV head, sequence, row block) spans, cut into tiles, form one line that is dealt out to the
+// workgroups in equal shares, whatever the sequences' lengths; a span that falls into several
+// shares leaves fp32 parts that a second launch joins (the merge of Appendix B, Equation 4).
+#include <math.h>
+
+#include "cp_common.h"
+
+namespace cp {
+namespace {
+
+#define CP_LDS_AS __attribute__((address_space(3)))
+#define CP_GLB_AS __attribute__((address_space(1)))
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef short shortx4_t __attribute__((ext_vector_type(4)));
+
+constexpr int SUB = 32;   // keys of a sub-tile
+
+// ---------------------------------------------------------------------------
+// The line of tiles
+// ---------------------------------------------------------------------------
+struct TreeParams {
+  const void* q;
+  const int32_t* q_pos;
+  const int32_t* cu_q;
+  const void* k_new;       // NULL: the tree's own keys are another rank's
+  const void* v_new;
+  const uint64_t* mask;    // [total_q][words]
+  const void* k;
+  const void* v;
+  const int32_t* kv_pos;
+  const int32_t* cu_kv;
+  const int32_t* used;     // or NULL: all slots of a sequence's range
+  void* out;
+  float* lse;
+  float* part_o;           // [2 * n_wg][row block][D], not normalised
+  float* part_ml;          // [2 * n_wg][row block][2]: running maximum (log2 domain), sum
+  int64_t total_q, total_kv;
+  int32_t batch, words, n_q_heads, n_kv_heads, group;
+  int32_t n_wg, min_share;
+  float scale_log2;
+};
+
+// What a sequence holds. Boundaries that contradict each other or the totals (they are read on the
+// device, where nothing can be refused) are cut to what is there.
+struct TreeSeq {
+  int64_t q0, k0;      // first node, first cache slot
+  int32_t n, used;     // nodes, tokens in the cache
+  int64_t spans, tiles;
+};
+__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
+  return x < lo ? lo : x > hi ? hi : x;
+}
+// RM rows of a row block, SPT sub-tiles of a tile
+template <int RM, int SPT>
+__device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
+  TreeSeq s;
+  s.q0 = clamp64(p.cu_q[b], 0, p.total_q);
+  s.n = (int32_t)(clamp64(p.cu_q[b + 1], s.q0, p.total_q) - s.q0);
+  s.k0 = clamp64(p.cu_kv[b], 0, p.total_kv);
+  const int64_t room = clamp64(p.cu_kv[b + 1], s.k0, p.total_kv) - s.k0;
+  s.used = (int32_t)(p.used != nullptr ? clamp64(p.used[b], 0, room) : room);
+  s.spans = ((int64_t)s.n * p.group + RM - 1) / RM;
+  const int64_t subs = (s.used + SUB - 1) / SUB + (p.k_new != nullptr ? (s.n + SUB - 1) / SUB : 0);
+  s.tiles = subs > 0 ? (subs + SPT - 1) / SPT : 1;   // (nothing to see: one tile, empty)
+  return s;
+}
+
+__device__ __forceinline__ int64_t wave_sum64(int64_t x) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+  return x;
+}
+
+// Tiles of one KV head.
+template <int RM, int SPT>
+__device__ __forceinline__ int64_t tree_total(const TreeParams& p) {
+  const int lane = threadIdx.x & 63;
+  int64_t sum = 0;
+  for (int b = lane; b < p.batch; b += 64) {
+    const TreeSeq s = tree_seq<RM, SPT>(p, b);
+    sum += s.spans * s.tiles;
+  }
+  return wave_sum64(sum);
+}
+
+// The sequence that tile u (of one KV head) belongs to, and the tile where it begins.
+template <int RM, int SPT>
+__device__ __forceinline__ int tree_find(const TreeParams& p, int64_t u, int64_t* begin) {
+  const int lane = threadIdx.x & 63;
+  int64_t base = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 64) {
+    int64_t c = 0;
+    if (b0 + lane < p.batch) {
+      const TreeSeq s = tree_seq<RM, SPT>(p, b0 + lane);
+      c = s.spans * s.tiles;
+    }
+    int64_t end = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t y = __shfl_up(end, o, 64);
+      if (lane >= o) end += y;
+    }
+    const uint64_t behind = __builtin_amdgcn_ballot_w64(base + end > u);
+    if (behind != 0) {
+      const int l = __builtin_ctzll(behind);
+      *begin = base + __shfl(end - c, l, 64);
+      return b0 + l;
+    }
+    base += __shfl(end, 63, 64);
+  }
+  *begin = base;
+  return -1;
+}
+
+// A workgroup's share of the line: as many tiles for each, `min_share` at least.
+__device__ __forceinline__ int64_t tree_share(const TreeParams& p, int64_t all) {
+  const int64_t s = (all + p.n_wg - 1) / p.n_wg;
+  return s < p.min_share ? p.min_share : s;
+}
+
+// ---------------------------------------------------------------------------
+// The kernel
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ floatx16_t mfma32(bf16x8_t a, bf16x8_t b, floatx16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16_t mfma32(float a, float b, floatx16_t c) {
+  return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void to_lds16(const void* src, char* dst_wave_uniform) {
+  __builtin_amdgcn_global_load_lds((const CP_GLB_AS void*)src, (CP_LDS_AS void*)dst_wave_uniform,
+                                   16, 0, 0);
+}
+__device__ __forceinline__ float xor32(float x) { return __shfl_xor(x, 32, 64); }
+
+// A sub-tile in LDS: 32 K rows, 32 V rows (16-byte chunks of a row permuted, see below), positions.
+template <typename TI, int D>
+struct SubTile {
+  static constexpr int ROW = D * (int)sizeof(TI);
+  static constexpr int CH = ROW / 16;              // 16-byte chunks of a row
+  static constexpr int V_OFF = SUB * ROW;
+  static constexpr int POS_OFF = 2 * SUB * ROW;
+  static constexpr int BYTES = POS_OFF + 256;
+  // Chunk c of K row r lies at c ^ k_perm(r): lanes that read the same chunk of neighbouring rows
+  // touch different banks. V of bf16: a transposed read takes 32 bytes of four neighbouring rows;
+  // chunk c lies at c ^ v_perm(r), which puts the 32-byte pieces of the four rows, and of the two
+  // 16-lane groups that read neighbouring channels, into different banks. (V of fp32 is read along
+  // its rows.)
+  __device__ static constexpr int k_perm(int r) { return r & (CH - 1); }
+  __device__ static constexpr int v_perm(int r) {
+    if (sizeof(TI) == 4) return 0;
+    return D == 128 ? (((r & 1) * 2) ^ (((r >> 1) & 1) * 5)) << 1 : (r & 3) << 1;
+  }
+};
+
+template <typename TO>
+__device__ __forceinline__ void store4(TO* dst, floatx4_t x);
+template <>
+__device__ __forceinline__ void store4<float>(float* dst, floatx4_t x) {
+  *(floatx4_t*)dst = x;
+}
+template <>
+__device__ __forceinline__ void store4<bf16_t>(bf16_t* dst, floatx4_t x) {
+  bf16x4_t y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = static_cast<bf16_t>(x[i]);
+  *(bf16x4_t*)dst = y;
+}
+
+// bf16 pairs: 1.0 where the element is not finite and not of sign `minus` (a NaN counts for both),
+// else 0; and the pair with what is not finite replaced by zero.
+__device__ __forceinline__ uint32_t not_finite(uint32_t x, bool minus) {
+  uint32_t r = 0;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t e = (x >> (16 * h)) & 0xffffu;
+    const bool nan = (e & 0x7fffu) > 0x7f80u;
+    if (nan || e == (minus ? 0xff80u : 0x7f80u)) r |= 0x3f80u << (16 * h);
+  }
+  return r;
+}
+__device__ __forceinline__ uint32_t only_finite(uint32_t x) {
+  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+  return x;
+}
+__device__ __forceinline__ bool any_not_finite(uint32_t x) {
+  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+}
+
+// KS: the wavefronts of a workgroup hold the same 32 C rows and take turns at the sub-tiles (few
+// rows: the keys are what there is to share out). Otherwise every wavefront holds 32 C rows of its
+// own and all read every sub-tile of a tile.
+template <bool KS, int C, int NW>
+struct Form {
+  static constexpr int RW = 32 * C;                    // rows of a wavefront
+  static constexpr int RM = KS ? RW : RW * NW;         // rows of a row block
+  static constexpr int SPT = KS ? NW : 2;              // sub-tiles of a tile
+};
+template <typename TI, int D, bool KS, int C, int NW>
+constexpr int tree_smem() {
+  using F = Form<KS, C, NW>;
+  const int tiles = F::SPT * SubTile<TI, D>::BYTES;
+  const int join = KS ? NW * (F::RW * (D + 4) + 2 * F::RW) * 4 : 0;
+  return tiles > join ? tiles : join;
+}
+
+// TI: K, V and Q. TO: O. P goes into the second product as TERMS bf16 terms (bf16 inputs): one
+// where O is rounded to bf16 itself, three (24 bits) where it stays fp32.
+template <typename TI, int D, bool KS, int C, int NW, int TERMS, typename TO>
+__global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) {
+  using F = Form<KS, C, NW>;
+  using T = SubTile<TI, D>;
+  constexpr bool F32 = sizeof(TI) == 4;
+  constexpr int NKS = T::ROW / 32, NCB = D / 32;
+  extern __shared__ __align__(16) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rl = lane & 31, hf = lane >> 5;   // row (N side) or key / channel (M side), half
+  const int64_t head_tiles = tree_total<F::RM, F::SPT>(p);
+  const int64_t all = head_tiles * p.n_kv_heads;
+  const int64_t share = tree_share(p, all);
+  int64_t u = blockIdx.x * share;
+  const int64_t u_end = min(all, u + share);
+  const int64_t tok_q = (int64_t)p.n_q_heads * D, tok_kv = (int64_t)p.n_kv_heads * D;
+
+  while (u < u_end) {
+    const int kvh = (int)(u / head_tiles);
+    int64_t begin;
+    const int b = tree_find<F::RM, F::SPT>(p, u - kvh * head_tiles, &begin);
+    if (b < 0) break;
+    const TreeSeq sq = tree_seq<F::RM, F::SPT>(p, b);
+    const int64_t in = u - kvh * head_tiles - begin;
+    const int64_t span = in / sq.tiles;
+    const int t0 = (int)(in - span * sq.tiles);
+    const int t1 = (int)min<int64_t>(sq.tiles, t0 + (u_end - u));
+    const int n_cached = (sq.used + SUB - 1) / SUB;
+    const int n_subs = n_cached + (p.k_new != nullptr ? (sq.n + SUB - 1) / SUB : 0);
+    const int64_t n_rows = (int64_t)sq.n * p.group;
+
+    // ---- the wavefront's rows ----
+    int64_t row[C];        // within (sequence, KV head)
+    int64_t node[C];       // of all nodes; -1: a row behind the last one
+    int32_t qp[C];
+    uint4 qf[C][NKS];      // lane (rl, hf): 16-byte chunk 2 ks + hf of row rl
+    int32_t q_min = INT32_MAX, q_max = INT32_MIN;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      row[c] = span * F::RM + (KS ? 0 : wave * F::RW) + c * 32 + rl;
+      const bool ok = row[c] < n_rows;
+      const int64_t nd = ok ? row[c] / p.group : 0;
+      node[c] = ok ? sq.q0 + nd : -1;
+      const int head = kvh * p.group + (ok ? (int)(row[c] - nd * p.group) : 0);
+      const uint4* src = (const uint4*)((const TI*)p.q + (ok ? node[c] : 0) * tok_q + head * D) + hf;
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {
+        qf[c][ks] = make_uint4(0, 0, 0, 0);
+        if (ok) qf[c][ks] = src[2 * ks];
+      }
+      qp[c] = ok ? p.q_pos[node[c]] : INT32_MIN;
+      if (ok) {
+        q_min = min(q_min, qp[c]);
+        q_max = max(q_max, qp[c]);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      q_min = min(q_min, __shfl_xor(q_min, o, 64));
+      q_max = max(q_max, __shfl_xor(q_max, o, 64));
+    }
+
+    float m_run[C], l_run[C];
+    floatx16_t o_acc[C][NCB];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      m_run[c] = -INFINITY;
+      l_run[c] = 0.f;
+#pragma unroll
+      for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o_acc[c][cb][i] = 0.f;
+    }
+
+    // Requests for sub-tile `st` into LDS at `dst`: rows behind its last one repeat that one (and are
+    // masked by their index). `w` of `nw` wavefronts share the requests out.
+    auto request = [&](int st, char* dst, int w, int nw) {
+      const bool own = st >= n_cached;
+      const int first = (own ? st - n_cached : st) * SUB;
+      const int last = min(SUB, (own ? sq.n : sq.used) - first) - 1;
+      const int64_t base = (own ? sq.q0 : sq.k0) + first;
+      const TI* kt = (const TI*)(own ? p.k_new : p.k) + base * tok_kv + kvh * D;
+      const TI* vt = (const TI*)(own ? p.v_new : p.v) + base * tok_kv + kvh * D;
+      constexpr int RPI = 64 / T::CH;          // rows of a request
+      for (int i = w; i < SUB / RPI; i += nw) {
+        const int r = i * RPI + lane / T::CH, slot = lane % T::CH;
+        const int64_t off = (int64_t)min(r, last) * tok_kv;
+        to_lds16((const uint4*)(kt + off) + (slot ^ T::k_perm(r)), dst + i * 1024);
+        to_lds16((const uint4*)(vt + off) + (slot ^ T::v_perm(r)), dst + T::V_OFF + i * 1024);
+      }
+      if (!own && w == 0)
+        __builtin_amdgcn_global_load_lds((const CP_GLB_AS void*)(p.kv_pos + base + min(rl, last)),
+                                         (CP_LDS_AS void*)(dst + T::POS_OFF), 4, 0, 0);
+    };
+
+    // S, P and O of one sub-tile that lies in LDS at `buf`.
+    auto compute = [&](int st, const char* buf) {
+      const bool own = st >= n_cached;
+      const int first = (own ? st - n_cached : st) * SUB;
+      const int cnt = min(SUB, (own ? sq.n : sq.used) - first);
+      bool masked = own || cnt < SUB;
+      if (!own) {
+        const int32_t kp = *(const int32_t*)(buf + T::POS_OFF + rl * 4);
+        if (__builtin_amdgcn_ballot_w64(kp <= q_max) == 0) return;   // none of the rows sees any
+        masked = masked || __builtin_amdgcn_ballot_w64(kp > q_min) != 0;
+      }
+      floatx16_t s[C];
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[c][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {
+        const uint4 a = *(const uint4*)(buf + rl * T::ROW + (((2 * ks + hf) ^ T::k_perm(rl)) << 4));
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          if constexpr (F32) {
+            const floatx4_t af = __builtin_bit_cast(floatx4_t, a);
+            const floatx4_t qv = __builtin_bit_cast(floatx4_t, qf[c][ks]);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s[c] = mfma32(af[x], qv[x], s[c]);
+          } else {
+            s[c] = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, qf[c][ks]),
+                          s[c]);
+          }
+        }
+      }
+      // score i of lane (rl, hf): key (i / 4) * 8 + hf * 4 + i % 4
+      bool odd_v = false;   // V holds what is not finite, which rows that do not see it must not meet
+      if (masked) {
+        const uint32_t there = cnt == SUB ? ~0u : (1u << cnt) - 1;
+        int32_t kp[16];
+        if (!own) {
+#pragma unroll
+          for (int a = 0; a < 4; ++a) {
+            const int4 x = *(const int4*)(buf + T::POS_OFF + (a * 8 + hf * 4) * 4);
+            kp[4 * a] = x.x; kp[4 * a + 1] = x.y; kp[4 * a + 2] = x.z; kp[4 * a + 3] = x.w;
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          uint32_t see = there;
+          if (own) {
+            const int word = (st - n_cached) >> 1;
+            see = 0;
+            if (node[c] >= 0 && word < p.words)
+              see = (uint32_t)(p.mask[node[c] * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const bool vis = ((see >> ((i >> 2) * 8 + hf * 4 + (i & 3))) & 1) != 0 &&
+                             (own || kp[i] <= qp[c]);
+            s[c][i] = vis ? s[c][i] : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < SUB * T::ROW / 1024; ++i) {
+          const uint4 x = *(const uint4*)(buf + T::V_OFF + i * 1024 + lane * 16);
+          if constexpr (F32)
+            odd_v |= (x.x & 0x7f800000u) == 0x7f800000u || (x.y & 0x7f800000u) == 0x7f800000u ||
+                     (x.z & 0x7f800000u) == 0x7f800000u || (x.w & 0x7f800000u) == 0x7f800000u;
+          else
+            odd_v |= any_not_finite(x.x) || any_not_finite(x.y) || any_not_finite(x.z) ||
+                     any_not_finite(x.w);
+        }
+        odd_v = __builtin_amdgcn_ballot_w64(odd_v) != 0;
+      }
+      u32x4_t pb[C][TERMS][2];   // P^T of keys 0..15 and 16..31, per term
+      float pf[C][F32 ? 16 : 1];
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float mx = s[c][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[c][i]);
+        mx = fmaxf(mx, xor32(mx));
+        const float m_new = fmaxf(m_run[c], mx * p.scale_log2);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = __builtin_amdgcn_exp2f(m_run[c] - m_use);
+        m_run[c] = m_new;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float e = __builtin_amdgcn_exp2f(fmaf(s[c][i], p.scale_log2, -m_use));
+          sum += e;
+          if constexpr (F32) {
+            pf[c][i] = e;
+          } else {
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) {
+              const bf16_t x = static_cast<bf16_t>(e);
+              const uint32_t bits = __builtin_bit_cast(uint16_t, x);
+              if ((i & 1) == 0) pb[c][t][i >> 3][(i & 7) >> 1] = bits;
+              else pb[c][t][i >> 3][(i & 7) >> 1] |= bits << 16;
+              e -= static_cast<float>(x);
+            }
+          }
+        }
+        l_run[c] = fmaf(l_run[c], alpha, sum);
+        if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+#pragma unroll
+          for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o_acc[c][cb][i] *= alpha;
+        }
+      }
+      if constexpr (F32) {
+        // O^T += V^T P^T, a key pair a step: k slot hf of step i is the key of score i
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb) {
+          floatx16_t plus[C], minus[C];   // how many visible infinities of either sign (a NaN: both)
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) plus[c][i] = minus[c][i] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int r = (i >> 2) * 8 + hf * 4 + (i & 3);
+            float v = *(const float*)(buf + T::V_OFF + r * T::ROW + (cb * 32 + rl) * 4);
+            if (odd_v) {
+              const bool fin = fabsf(v) < INFINITY;
+              const float up = fin || v == -INFINITY ? 0.f : 1.f, dn = fin || v == INFINITY ? 0.f : 1.f;
+#pragma unroll
+              for (int c = 0; c < C; ++c) {
+                const float seen = pf[c][i] != 0.f ? 1.f : 0.f;
+                plus[c] = mfma32(up, seen, plus[c]);
+                minus[c] = mfma32(dn, seen, minus[c]);
+              }
+              v = fin ? v : 0.f;
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) o_acc[c][cb] = mfma32(v, pf[c][i], o_acc[c][cb]);
+          }
+          if (odd_v) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                o_acc[c][cb][i] += (plus[c][i] > 0.f ? INFINITY : 0.f) + (minus[c][i] > 0.f ? -INFINITY : 0.f);
+          }
+        }
+      } else {
+        // O^T += V^T P^T: k slot j of half hf in step kb is key kb*16 + (j/4)*8 + hf*4 + j%4
+        const int vj = (lane & 15) >> 2, vq = lane & 3, vg = (lane >> 4) & 1;
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb) {
+          u32x4_t v[2];
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int r = kb * 16 + x * 8 + hf * 4 + vj;
+              const int chunk = cb * 4 + vg * 2 + (vq >> 1);
+              const char* at = buf + T::V_OFF + r * T::ROW + ((chunk ^ T::v_perm(r)) << 4) + (vq & 1) * 8;
+              const u32x2_t z = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                                (CP_LDS_AS shortx4_t*)at));
+              v[kb][2 * x] = z[0];
+              v[kb][2 * x + 1] = z[1];
+            }
+          if (__builtin_expect(odd_v, 0)) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+              floatx16_t sign[2];   // how many visible infinities of either sign (a NaN: both)
+#pragma unroll
+              for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sign[m][i] = 0.f;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                  u32x4_t a, seen;
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) {
+                    a[x] = not_finite(v[kb][x], m == 1);
+                    seen[x] = ((pb[c][0][kb][x] & 0xffffu) != 0 ? 0x3f80u : 0) |
+                              ((pb[c][0][kb][x] >> 16) != 0 ? 0x3f800000u : 0);
+                  }
+                  sign[m] = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, seen),
+                                   sign[m]);
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                o_acc[c][cb][i] += (sign[0][i] > 0.f ? INFINITY : 0.f) + (sign[1][i] > 0.f ? -INFINITY : 0.f);
+            }
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) v[kb][x] = only_finite(v[kb][x]);
+          }
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+              for (int t = 0; t < TERMS; ++t)
+                o_acc[c][cb] = mfma32(__builtin_bit_cast(bf16x8_t, v[kb]),
+                                      __builtin_bit_cast(bf16x8_t, pb[c][t][kb]), o_acc[c][cb]);
+        }
+      }
+    };
+
+    for (int t = t0; t < t1; ++t) {
+      __syncthreads();   // the tile before has been read
+      if (KS) {
+        const int st = t * F::SPT + wave;
+        if (st < n_subs) request(st, smem + wave * T::BYTES, 0, 1);
+      } else {
+        for (int x = 0; x < F::SPT; ++x)
+          if (t * F::SPT + x < n_subs) request(t * F::SPT + x, smem + x * T::BYTES, wave, NW);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (KS) {
+        const int st = t * F::SPT + wave;
+        if (st < n_subs) compute(st, smem + wave * T::BYTES);
+      } else {
+        for (int x = 0; x < F::SPT; ++x)
+          if (t * F::SPT + x < n_subs) compute(t * F::SPT + x, smem + x * T::BYTES);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) l_run[c] += xor32(l_run[c]);
+
+    // ---- the span's result, or this share's part of it ----
+    const bool whole = t0 == 0 && t1 == sq.tiles;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
+    auto write = [&](int64_t r, int in_block, float m, float l, int ch, floatx4_t o4) {
+      if (r >= n_rows) return;
+      if (whole) {
+        const int64_t nd = r / p.group;
+        const int64_t at = (sq.q0 + nd) * p.n_q_heads + kvh * p.group + (r - nd * p.group);
+        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;   // (a NaN stays one)
+        store4<TO>((TO*)p.out + at * D + ch, o4 * inv);
+        if (ch == 0) p.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      } else {
+        const int64_t at = slot * F::RM + in_block;
+        *(floatx4_t*)(p.part_o + at * D + ch) = o4;
+        if (ch == 0) {
+          p.part_ml[at * 2] = m;
+          p.part_ml[at * 2 + 1] = l;
+        }
+      }
+    };
+    if constexpr (KS) {
+      // the wavefronts' disjoint subsets of the keys are joined in LDS
+      constexpr int OS = D + 4;                      // floats of a row
+      constexpr int WS = F::RW * OS + 2 * F::RW;     // of a wavefront
+      float* const cb0 = (float*)smem;
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float* const mine = cb0 + wave * WS + (c * 32 + rl) * OS;
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+            *(floatx4_t*)(mine + cb * 32 + a * 8 + hf * 4) =
+                floatx4_t{o_acc[c][cb][4 * a], o_acc[c][cb][4 * a + 1], o_acc[c][cb][4 * a + 2],
+                          o_acc[c][cb][4 * a + 3]};
+        if (hf == 0) {
+          cb0[wave * WS + F::RW * OS + c * 32 + rl] = m_run[c];
+          cb0[wave * WS + F::RW * OS + F::RW + c * 32 + rl] = l_run[c];
+        }
+      }
+      __syncthreads();
+      for (int e = tid; e < F::RW * (D / 4); e += NW * 64) {
+        const int r = e / (D / 4), ch = (e % (D / 4)) * 4;
+        float m = -INFINITY, l = 0.f;
+        floatx4_t o4 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, cb0[w * WS + F::RW * OS + r]);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          const float lw = cb0[w * WS + F::RW * OS + F::RW + r];
+          const float f = m == -INFINITY ? lw   // (0, or a NaN)
+                                         : __builtin_amdgcn_exp2f(cb0[w * WS + F::RW * OS + r] - m);
+          const floatx4_t x = *(const floatx4_t*)(cb0 + w * WS + r * OS + ch);
+          l = fmaf(lw, f, l);
+          o4 += x * f;
+        }
+        write(span * F::RM + r, r, m, l, ch, o4);
+      }
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+            write(row[c], wave * F::RW + c * 32 + rl, m_run[c], l_run[c], cb * 32 + a * 8 + hf * 4,
+                  floatx4_t{o_acc[c][cb][4 * a], o_acc[c][cb][4 * a + 1], o_acc[c][cb][4 * a + 2],
+                            o_acc[c][cb][4 * a + 3]});
+    }
+    u += t1 - t0;
+  }
+}
+
+// Joins the parts of the spans that fell into several shares: a wavefront per row.
+template <int D, int RM, int SPT, typename TO>
+__global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
+  constexpr int V = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t all_rows = p.total_q * p.n_q_heads;
+  const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (idx >= all_rows) return;
+  const int64_t node = idx / p.n_q_heads;
+  const int head = (int)(idx - node * p.n_q_heads), kvh = head / p.group;
+  // the sequence of this node and the tiles before it
+  int64_t before = 0, total = 0;
+  int b = -1;
+  for (int b0 = 0; b0 < p.batch; b0 += 64) {
+    int64_t c = 0;
+    bool mine = false;
+    if (b0 + lane < p.batch) {
+      const TreeSeq s = tree_seq<RM, SPT>(p, b0 + lane);
+      c = s.spans * s.tiles;
+      mine = node >= s.q0 && node < s.q0 + s.n;
+    }
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(mine);
+    if (b < 0 && hit != 0) {
+      const int l = __builtin_ctzll(hit);
+      b = b0 + l;
+      before = total + wave_sum64(lane < l ? c : 0);
+    }
+    total += wave_sum64(c);
+  }
+  if (b < 0) return;   // behind the last tree
+  const TreeSeq s = tree_seq<RM, SPT>(p, b);
+  const int64_t row = (node - s.q0) * p.group + (head - kvh * p.group);
+  const int64_t span = row / RM;
+  const int64_t a = kvh * total + before + span * s.tiles, e = a + s.tiles;
+  const int64_t share = tree_share(p, total * p.n_kv_heads);
+  const int64_t w0 = a / share, w1 = (e - 1) / share;
+  if (w0 == w1) return;
+  float m = -INFINITY, l = 0.f, o[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) o[i] = 0.f;
+  for (int64_t w = w0; w <= w1; ++w) {
+    const int64_t at = (2 * w + (w == w0 ? 1 : 0)) * RM + (row - span * RM);
+    const float mw = p.part_ml[at * 2], lw = p.part_ml[at * 2 + 1];
+    if (lw == 0.f) continue;
+    const float mn = fmaxf(m, mw);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    const float fw = __builtin_amdgcn_exp2f(mw - mn);
+    m = mn;
+    l = fmaf(l, f, lw * fw);
+#pragma unroll
+    for (int i = 0; i < V; ++i) o[i] = fmaf(o[i], f, p.part_o[at * D + lane * V + i] * fw);
+  }
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+#pragma unroll
+  for (int i = 0; i < V; ++i) ((TO*)p.out)[idx * D + lane * V + i] = from_float<TO>(o[i] * inv);
+  if (lane == 0) p.lse[idx] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------
+// Commit of the accepted paths: a workgroup per sequence lists the nodes that the accepted node's
+// mask names and copies their rows behind what the cache holds. Pure data movement of a few rows,
+// bound by its chain of latencies {accepted, used} -> mask -> rows.
+// ---------------------------------------------------------------------------
+struct AcceptParams {
+  const uint4* k_new;
+  const uint4* v_new;
+  const int32_t* pos_new;
+  const int32_t* cu_new;
+  const uint64_t* mask;
+  const int32_t* accepted;
+  uint4* k;
+  uint4* v;
+  int32_t* kv_pos;
+  const int32_t* cu_kv;
+  int32_t* used;
+  int32_t* dropped;
+  int64_t total_new, slots;
+  int32_t words, chunks;   // 16-byte chunks of a row
+};
+constexpr int ACCEPT_THREADS = 256;
+
+__global__ __launch_bounds__(ACCEPT_THREADS) void tree_accept_kernel(const AcceptParams p) {
+  __shared__ int16_t path[CP_TREE_MAX_WORDS * 64];
+  __shared__ int count;
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int64_t q0 = clamp64(p.cu_new[b], 0, p.total_new);
+  const int64_t n = clamp64(p.cu_new[b + 1], q0, p.total_new) - q0;
+  const int64_t k0 = clamp64(p.cu_kv[b], 0, p.slots);
+  const int64_t room = clamp64(p.cu_kv[b + 1], k0, p.slots) - k0;
+  const int64_t used = clamp64(p.used[b], 0, room);
+  const int acc = p.accepted[b];
+  if (acc < 0 || acc >= n) return;   // uniform
+  if (tid < 64) {   // a word a lane
+    uint64_t m = tid < p.words ? p.mask[(q0 + acc) * p.words + tid] : 0;
+    const int64_t left = n - tid * 64;
+    if (left < 64) m &= left > 0 ? (1ull << left) - 1 : 0;
+    const int c = __builtin_popcountll(m);
+    int end = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(end, o, 64);
+      if (tid >= o) end += y;
+    }
+    int at = end - c;
+    for (; m != 0; m &= m - 1) path[at++] = (int16_t)(tid * 64 + __builtin_ctzll(m));
+    if (tid == 63) count = end;
+  }
+  __syncthreads();
+  const int taken = (int)min<int64_t>(count, room - used);
+  for (int e = tid; e < taken * p.chunks; e += ACCEPT_THREADS) {
+    const int i = e / p.chunks, c = e - i * p.chunks;
+    const int64_t src = (q0 + path[i]) * p.chunks + c, dst = (k0 + used + i) * p.chunks + c;
+    p.k[dst] = p.k_new[src];
+    p.v[dst] = p.v_new[src];
+  }
+  for (int i = tid; i < taken; i += ACCEPT_THREADS) p.kv_pos[k0 + used + i] = p.pos_new[q0 + path[i]];
+  if (tid == 0) {   // (every thread has read used[b] before the barrier above)
+    if (taken > 0) p.used[b] = (int32_t)(used + taken);
+    if (p.dropped != nullptr && count > taken) atomicAdd(p.dropped, count - taken);
+  }
+}
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+enum TreeForm { kFew32, kFew64, kMany };
+struct TreePlan {
+  TreeForm form;
+  int rm, spt, n_wg, min_share;
+  size_t o_bytes, ml_bytes;
+};
+constexpr int kManyWaves = 8;
+
+TreePlan tree_plan(const cp_shape& s) {
+  TreePlan pl = {};
+  const int64_t group = s.n_q_heads / s.n_kv_heads;
+  const int64_t rows = s.total_q * group / s.batch;   // of a sequence, on average
+  pl.form = s.dtype == CP_FP32 || rows <= 32 ? kFew32 : rows <= 128 ? kFew64 : kMany;
+  pl.rm = pl.form == kFew32 ? 32 : pl.form == kFew64 ? 64 : 32 * kManyWaves;
+  pl.spt = pl.form == kMany ? 2 : 4;
+  pl.min_share = 1;
+  // no more workgroups than there can be tiles
+  const int64_t spans = s.total_q * group / pl.rm + s.batch;
+  const int64_t tiles = (s.total_kv + s.total_q) / (SUB * pl.spt) + 2 * (int64_t)s.batch;
+  const int64_t most = pl.form == kMany ? 256 : 512;
+  const int64_t any = spans > most || tiles > most ? most : spans * tiles * s.n_kv_heads;
+  pl.n_wg = (int)(any < most ? any : most);
+  pl.o_bytes = round256((size_t)2 * pl.n_wg * pl.rm * s.head_dim * 4);
+  pl.ml_bytes = round256((size_t)2 * pl.n_wg * pl.rm * 2 * 4);
+  return pl;
+}
+
+template <typename TI, int D, bool KS, int C, int NW, int TERMS, typename TO>
+int launch_form(const TreeParams& p, hipStream_t st) {
+  using F = Form<KS, C, NW>;
+  constexpr int smem = tree_smem<TI, D, KS, C, NW>();
+  static_assert(smem <= 160 * 1024, "LDS of a CU");
+  auto kernel = tree_attn_kernel<TI, D, KS, C, NW, TERMS, TO>;
+  if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, smem) !=
+      hipSuccess)
+    return CP_ERR_LAUNCH;
+  hipLaunchKernelGGL(kernel, dim3(p.n_wg), dim3(NW * 64), smem, st, p);
+  if (check_launch() != CP_OK) return CP_ERR_LAUNCH;
+  const int64_t rows = p.total_q * p.n_q_heads;
+  hipLaunchKernelGGL((tree_join_kernel<D, F::RM, F::SPT, TO>), dim3((unsigned)((rows + 3) / 4)),
+                     dim3(256), 0, st, p);
+  return check_launch();
+}
+
+template <int D, int TERMS, typename TO>
+int launch_bf16(const TreeParams& p, TreeForm form, hipStream_t st) {
+  switch (form) {
+    case kFew32: return launch_form<bf16_t, D, true, 1, 4, TERMS, TO>(p, st);
+    case kFew64: return launch_form<bf16_t, D, true, 2, 4, TERMS, TO>(p, st);
+    default: return launch_form<bf16_t, D, false, 1, kManyWaves, TERMS, TO>(p, st);
+  }
+}
+
+}  // namespace
+
+size_t tree_workspace_bytes(const cp_shape& s) {
+  if (s.total_q == 0) return 0;
+  const TreePlan pl = tree_plan(s);
+  return pl.o_bytes + pl.ml_bytes;
+}
+
+}  // namespace cp
+
+extern "C" {
+
+int cp_tree_mask(int32_t batch, const int32_t* cu_seqlens, const int32_t* parents, int32_t mask_words,
+                 uint64_t* mask_out) {
+  if (cu_seqlens == nullptr) return CP_ERR_NULL;
+  if (batch < 1 || mask_words < 1 || mask_words > CP_TREE_MAX_WORDS || cu_seqlens[0] != 0)
+    return CP_ERR_SHAPE;
+  for (int b = 0; b < batch; ++b) {
+    const int64_t n = (int64_t)cu_seqlens[b + 1] - cu_seqlens[b];
+    if (n < 0 || n > 64 * (int64_t)mask_words) return CP_ERR_SHAPE;
+  }
+  if (cu_seqlens[batch] > 0 && (parents == nullptr || mask_out == nullptr)) return CP_ERR_NULL;
+  for (int b = 0; b < batch; ++b)
+    for (int32_t i = 0; i < cu_seqlens[b + 1] - cu_seqlens[b]; ++i) {
+      const int32_t parent = parents[cu_seqlens[b] + i];
+      if (parent < -1 || parent >= i) return CP_ERR_SHAPE;
+    }
+  for (int b = 0; b < batch; ++b) {
+    uint64_t* const tree = mask_out + (int64_t)cu_seqlens[b] * mask_words;
+    for (int32_t i = 0; i < cu_seqlens[b + 1] - cu_seqlens[b]; ++i) {
+      const int32_t parent = parents[cu_seqlens[b] + i];
+      uint64_t* const m = tree + (int64_t)i * mask_words;
+      for (int w = 0; w < mask_words; ++w)
+        m[w] = parent < 0 ? 0 : tree[(int64_t)parent * mask_words + w];
+      m[i / 64] |= 1ull << (i % 64);
+    }
+  }
+  return CP_OK;
+}
+
+int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
+                 const int32_t* cu_seqlens_q, const void* k_new, const void* v_new,
+                 const uint64_t* tree_mask, int32_t mask_words, const void* k_cache,
+                 const void* v_cache, const int32_t* kv_pos_cache, const int32_t* cu_seqlens_kv,
+                 const int32_t* seq_used, void* out, float* lse, int32_t out_dtype, void* workspace,
+                 size_t workspace_bytes, void* stream) {
+  using namespace cp;
+  const int rc = check_shape(shape);
+  if (rc != CP_OK) return rc;
+  const cp_shape& s = *shape;
+  if (out_dtype != CP_BF16 && out_dtype != CP_FP32) return CP_ERR_UNSUPPORTED;
+  if ((k_new == nullptr) != (v_new == nullptr)) return CP_ERR_NULL;
+  if (k_new != nullptr && (mask_words < 1 || mask_words > CP_TREE_MAX_WORDS)) return CP_ERR_SHAPE;
+  if (cu_seqlens_q == nullptr || cu_seqlens_kv == nullptr) return CP_ERR_NULL;
+  if (s.total_q > 0 && (q == nullptr || q_pos == nullptr || out == nullptr || lse == nullptr))
+    return CP_ERR_NULL;
+  if (s.total_q > 0 && k_new != nullptr && tree_mask == nullptr) return CP_ERR_NULL;
+  if (s.total_q > 0 && s.total_kv > 0 &&
+      (k_cache == nullptr || v_cache == nullptr || kv_pos_cache == nullptr))
+    return CP_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) ||
+      !aligned16(v_cache) || !aligned16(out))
+    return CP_ERR_ALIGN;
+  if (s.total_q == 0) return CP_OK;
+  // rows of the merge's grid, nodes and tokens of a sequence with their sub-tiles are kept in 31 bits
+  if (s.total_q * s.n_q_heads > INT32_MAX || s.total_kv > INT32_MAX - SUB || s.batch > (1 << 24))
+    return CP_ERR_SHAPE;
+  const TreePlan pl = tree_plan(s);
+  if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 ||
+      workspace_bytes < pl.o_bytes + pl.ml_bytes)
+    return CP_ERR_WORKSPACE;
+  TreeParams p = {};
+  p.q = q; p.q_pos = q_pos; p.cu_q = cu_seqlens_q;
+  p.k_new = k_new; p.v_new = v_new; p.mask = tree_mask; p.words = mask_words;
+  p.k = k_cache; p.v = v_cache; p.kv_pos = kv_pos_cache; p.cu_kv = cu_seqlens_kv; p.used = seq_used;
+  p.out = out; p.lse = lse;
+  p.part_o = (float*)workspace;
+  p.part_ml = (float*)((char*)workspace + pl.o_bytes);
+  p.total_q = s.total_q; p.total_kv = s.total_kv; p.batch = s.batch;
+  p.n_q_heads = s.n_q_heads; p.n_kv_heads = s.n_kv_heads; p.group = s.n_q_heads / s.n_kv_heads;
+  p.n_wg = pl.n_wg; p.min_share = pl.min_share;
+  p.scale_log2 = (s.softmax_scale > 0.f ? s.softmax_scale : 1.0f / sqrtf((float)s.head_dim)) * kLog2e;
+  hipStream_t st = (hipStream_t)stream;
+  const bool f32_out = out_dtype == CP_FP32;
+  if (s.dtype == CP_FP32) {
+    if (s.head_dim == 64)
+      return f32_out ? launch_form<float, 64, true, 1, 4, 1, float>(p, st)
+                     : launch_form<float, 64, true, 1, 4, 1, bf16_t>(p, st);
+    return f32_out ? launch_form<float, 128, true, 1, 4, 1, float>(p, st)
+                   : launch_form<float, 128, true, 1, 4, 1, bf16_t>(p, st);
+  }
+  if (s.head_dim == 64)
+    return f32_out ? launch_bf16<64, 3, float>(p, pl.form, st) : launch_bf16<64, 1, bf16_t>(p, pl.form, st);
+  return f32_out ? launch_bf16<128, 3, float>(p, pl.form, st) : launch_bf16<128, 1, bf16_t>(p, pl.form, st);
+}
+
+int cp_tree_accept(const cp_shape* shape, const void* k_new, const void* v_new,
+                   const int32_t* pos_new, const int32_t* cu_seqlens_new, const uint64_t* tree_mask,
+                   int32_t mask_words, const int32_t* accepted, void* k_cache, void* v_cache,
+                   int32_t* kv_pos_cache, const int32_t* cu_seqlens_kv, int32_t* seq_used,
+                   int32_t* dropped, void* stream) {
+  using namespace cp;
+  const int rc = check_cache_shape(shape);
+  if (rc != CP_OK) return rc;
+  const cp_shape& s = *shape;
+  if (mask_words < 1 || mask_words > CP_TREE_MAX_WORDS) return CP_ERR_SHAPE;
+  if (cu_seqlens_new == nullptr || cu_seqlens_kv == nullptr || seq_used == nullptr ||
+      accepted == nullptr)
+    return CP_ERR_NULL;
+  if (s.total_q > 0 && (k_new == nullptr || v_new == nullptr || pos_new == nullptr ||
+                        tree_mask == nullptr))
+    return CP_ERR_NULL;
+  if (s.total_q > 0 && s.total_kv > 0 &&
+      (k_cache == nullptr || v_cache == nullptr || kv_pos_cache == nullptr))
+    return CP_ERR_NULL;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) || !aligned16(v_cache))
+    return CP_ERR_ALIGN;
+  if (s.total_q == 0) return CP_OK;
+  AcceptParams p;
+  p.k_new = (const uint4*)k_new; p.v_new = (const uint4*)v_new;
+  p.pos_new = pos_new; p.cu_new = cu_seqlens_new; p.mask = tree_mask; p.accepted = accepted;
+  p.k = (uint4*)k_cache; p.v = (uint4*)v_cache; p.kv_pos = kv_pos_cache; p.cu_kv = cu_seqlens_kv;
+  p.used = seq_used; p.dropped = dropped;
+  p.total_new = s.total_q; p.slots = s.total_kv; p.words = mask_words;
+  const int64_t chunks = (int64_t)s.n_kv_heads * s.head_dim * (s.dtype == CP_BF16 ? 2 : 4) / 16;
+  // a path's chunks are counted in 31 bits
+  if (chunks * CP_TREE_MAX_WORDS * 64 > INT32_MAX) return CP_ERR_SHAPE;
+  p.chunks = (int32_t)chunks;
+  hipLaunchKernelGGL(tree_accept_kernel, dim3((unsigned)s.batch), dim3(ACCEPT_THREADS), 0,
+                     (hipStream_t)stream, p);
+  return check_launch();
+}
+
+}  // extern "C"

@@ -25,6 +25,13 @@ struct Functions {
   decltype(&cp_ring_passkv) ring[3];  // pass-KV, pass-Q, pass-Q decode
 } fn = {};
 
+struct CacheFunctions {
+  decltype(&cp_tree_attn) tree_attn;
+  decltype(&cp_tree_accept) tree_accept;
+  decltype(&cp_kv_attn_weight) weight;
+  decltype(&cp_kv_evict) evict;
+} cache_fn = {};
+
 PyObject* get_device = nullptr;      // torch._C._cuda_getDevice
 PyObject* get_raw_stream = nullptr;  // torch._C._cuda_getCurrentRawStream
 
@@ -305,6 +312,195 @@ PyObject* append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- calls on the KV cache: trees of drafted tokens, attention weight, eviction ----
+
+void cache_arguments(Py_ssize_t n, Py_ssize_t want) {
+  arguments(n, want);
+  if (cache_fn.tree_attn == nullptr) raise(PyExc_RuntimeError, "the library is not loaded");
+}
+// What a tensor has to be; `numel` < 0: any number of elements.
+const at::Tensor& checked(PyObject* o, at::ScalarType type, int64_t numel, const char* name) {
+  const at::Tensor& t = tensor(o);
+  if (t.scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "%s must be %s", name, at::toString(type));
+    throw Raised{};
+  }
+  if (numel >= 0 && t.numel() != numel) {
+    PyErr_Format(PyExc_ValueError, "%s has the wrong number of elements", name);
+    throw Raised{};
+  }
+  return t;
+}
+int32_t* ints(PyObject* o, int64_t numel, const char* name) {
+  return (int32_t*)pointer(checked(o, at::kInt, numel, name));
+}
+// All tensors of a call lie on the current GPU, whose stream the call is made on.
+void on_current_device(PyObject* const* a, std::initializer_list<int> which) {
+  PyObject* const dev = PyObject_CallNoArgs(get_device);
+  if (dev == nullptr) throw Raised{};
+  const long current = PyLong_AsLong(dev);
+  Py_DECREF(dev);
+  if (current == -1 && PyErr_Occurred()) throw Raised{};
+  for (const int i : which) {
+    if (a[i] == Py_None) continue;
+    const at::Tensor& t = tensor(a[i]);
+    if (!t.is_cuda() || t.get_device() != current)
+      raise(PyExc_ValueError, "tensors must be on the current GPU");
+  }
+}
+void same_rows(const at::Tensor& x, const at::Tensor& cache, const char* what) {
+  if (x.dim() != 3) raise(PyExc_ValueError, what);
+  if (x.scalar_type() != cache.scalar_type() || x.size(1) != cache.size(1) ||
+      x.size(2) != cache.size(2))
+    raise(PyExc_ValueError, what);
+}
+// K rows of a cache in a[i], V, positions, boundaries and counts behind it; the shape of a call on it.
+cp_shape cache_shape(PyObject* const* a, int i) {
+  const at::Tensor &k = tensor(a[i]), &cu = checked(a[i + 3], at::kInt, -1, "cu_seqlens_kv");
+  if (k.dim() != 3) raise(PyExc_ValueError, "a cache's K must have three dimensions");
+  same_rows(tensor(a[i + 1]), k, "K and V of the cache differ in shape or dtype");
+  if (tensor(a[i + 1]).size(0) != k.size(0)) raise(PyExc_ValueError, "K and V of the cache differ in length");
+  checked(a[i + 2], at::kInt, k.size(0), "kv_pos of the cache");
+  checked(a[i + 4], at::kInt, cu.numel(), "used of the cache");
+  cp_shape s = {};
+  s.dtype = dtype_code(k.scalar_type());
+  s.head_dim = (int32_t)k.size(2);
+  s.n_q_heads = s.n_kv_heads = (int32_t)k.size(1);
+  s.batch = (int32_t)cu.numel() - 1;
+  s.total_kv = k.size(0);
+  return s;
+}
+void queries(cp_shape& s, const at::Tensor& q, const at::Tensor& cache, float scale) {
+  if (q.dim() != 3) raise(PyExc_ValueError, "q must have three dimensions");
+  if (q.scalar_type() != cache.scalar_type() || q.size(2) != cache.size(2))
+    raise(PyExc_ValueError, "q does not match the cache's head_dim or dtype");
+  s.n_q_heads = (int32_t)q.size(1);
+  s.total_q = q.size(0);
+  s.softmax_scale = scale;
+}
+// Words of a node's mask.
+int32_t mask_words(PyObject* o, int64_t nodes) {
+  const at::Tensor& m = checked(o, at::kLong, -1, "tree_mask");
+  if (m.dim() != 2 || m.size(0) != nodes)
+    raise(PyExc_ValueError, "tree_mask must be [nodes, words] of int64");
+  return (int32_t)m.size(1);
+}
+
+// q, q_pos, cu_seqlens_q, k_new, v_new, tree_mask, k, v, kv_pos, cu, used (of the cache), out_dtype,
+// scale, out, lse, workspace, stream
+PyObject* tree_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    cache_arguments(n, 17);
+    const at::Tensor &q = tensor(a[0]), &k = tensor(a[6]);
+    cp_shape s = cache_shape(a, 6);
+    queries(s, q, k, number(a[12]));
+    int32_t words = 0;
+    if ((a[3] == Py_None) != (a[4] == Py_None) || (a[3] == Py_None) != (a[5] == Py_None))
+      raise(PyExc_ValueError, "k_new, v_new and tree_mask come together");
+    if (a[3] != Py_None) {
+      for (int i = 3; i < 5; ++i) {
+        same_rows(tensor(a[i]), k, "k_new / v_new do not match the cache's row shape or dtype");
+        if (tensor(a[i]).size(0) != s.total_q) raise(PyExc_ValueError, "a row of k_new and v_new per node");
+      }
+      words = mask_words(a[5], s.total_q);
+    }
+    int32_t* const q_pos = ints(a[1], s.total_q, "q_pos");
+    int32_t* const cu_q = ints(a[2], s.batch + 1, "cu_seqlens_q");
+    if (a[13] != Py_None && tensor(a[13]).numel() != q.numel())
+      raise(PyExc_ValueError, "out has the wrong number of elements");
+    if (a[14] != Py_None) checked(a[14], at::kFloat, s.total_q * s.n_q_heads, "lse");
+    on_current_device(a, {0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 13, 14, 15});
+    const at::Tensor out = result(a[13], q.sizes(), q, dtype_or(a[11], q.scalar_type()));
+    const at::Tensor lse = result(a[14], {q.size(0), q.size(1)}, q, at::kFloat);
+    Workspace w;
+    use_workspace(w, a[15], s, CP_WS_TREE, q);
+    const int rc = call(cache_fn.tree_attn, &s, pointer(q), q_pos, cu_q, pointer(a[3]), pointer(a[4]),
+                        (const uint64_t*)pointer(a[5]), words, pointer(k), pointer(a[7]),
+                        (int32_t*)pointer(a[8]), (int32_t*)pointer(a[9]), (int32_t*)pointer(a[10]),
+                        pointer(out), (float*)pointer(lse), dtype_code(out.scalar_type()), w.ptr,
+                        w.bytes, stream_of(a[16]));
+    return rc != CP_OK ? status(rc) : pair(object(a[13], out), object(a[14], lse));
+  });
+}
+
+// k_new, v_new, pos_new, cu_seqlens_new, tree_mask, accepted, k, v, kv_pos, cu, used, dropped (of the
+// cache), stream
+PyObject* tree_accept(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    cache_arguments(n, 13);
+    const at::Tensor &k_new = tensor(a[0]), &k = tensor(a[6]);
+    cp_shape s = cache_shape(a, 6);
+    for (int i = 0; i < 2; ++i)
+      same_rows(tensor(a[i]), k, "k_new / v_new do not match the cache's row shape or dtype");
+    s.total_q = k_new.size(0);
+    if (tensor(a[1]).size(0) != s.total_q) raise(PyExc_ValueError, "a row of k_new and v_new per node");
+    const int32_t words = mask_words(a[4], s.total_q);
+    int32_t* const pos = ints(a[2], s.total_q, "pos_new");
+    int32_t* const cu = ints(a[3], s.batch + 1, "cu_seqlens_new");
+    int32_t* const accepted = ints(a[5], s.batch, "accepted");
+    int32_t* const dropped = ints(a[11], 1, "dropped");
+    on_current_device(a, {0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 10, 11});
+    return status(call(cache_fn.tree_accept, &s, pointer(k_new), pointer(a[1]), pos, cu,
+                       (const uint64_t*)pointer(a[4]), words, accepted, pointer(k), pointer(a[7]),
+                       (int32_t*)pointer(a[8]), (int32_t*)pointer(a[9]), (int32_t*)pointer(a[10]),
+                       dropped, stream_of(a[12])));
+  });
+}
+
+// q, q_pos, cu_seqlens_q, lse, weight, k, v, kv_pos, cu, used (of the cache), decay, scale, workspace,
+// stream
+PyObject* kv_weight(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    cache_arguments(n, 14);
+    const at::Tensor &q = tensor(a[0]), &k = tensor(a[5]);
+    cp_shape s = cache_shape(a, 5);
+    queries(s, q, k, number(a[11]));
+    const float decay = number(a[10]);
+    int32_t* const q_pos = ints(a[1], s.total_q, "q_pos");
+    int32_t* const cu_q = ints(a[2], s.batch + 1, "cu_seqlens_q");
+    const at::Tensor& lse = checked(a[3], at::kFloat, s.total_q * s.n_q_heads, "lse");
+    const at::Tensor& weight = checked(a[4], at::kFloat, s.total_kv, "weight");
+    on_current_device(a, {0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 12});
+    Workspace w;
+    use_workspace(w, a[12], s, CP_WS_WEIGHT, q);
+    return status(call(cache_fn.weight, &s, pointer(q), q_pos, cu_q, (float*)pointer(lse), pointer(k),
+                       (int32_t*)pointer(a[7]), (int32_t*)pointer(a[8]), (int32_t*)pointer(a[9]), decay,
+                       (float*)pointer(weight), w.ptr, w.bytes, stream_of(a[13])));
+  });
+}
+
+// k, v, kv_pos, cu, used (of the cache), weight, budget, protect_from, sinks, the same six of the
+// destination or None, workspace, stream
+PyObject* kv_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    cache_arguments(n, 17);
+    const at::Tensor& k = tensor(a[0]);
+    const cp_shape s = cache_shape(a, 0);
+    const at::Tensor& weight = checked(a[5], at::kFloat, s.total_kv, "weight");
+    int32_t* const budget = ints(a[6], s.batch, "budget");
+    int32_t* const protect = a[7] == Py_None ? nullptr : ints(a[7], s.batch, "protect_from");
+    const long sinks = PyLong_AsLong(a[8]);
+    if (sinks == -1 && PyErr_Occurred()) throw Raised{};
+    if (sinks < 0 || sinks > INT32_MAX) raise(PyExc_ValueError, "sinks must be a count of positions");
+    int64_t slots_to = 0;
+    if (a[9] != Py_None) {
+      const cp_shape d = cache_shape(a, 9);
+      same_rows(tensor(a[9]), k, "the caches differ in row shape or dtype");
+      if (d.batch != s.batch) raise(PyExc_ValueError, "the caches differ in their number of sequences");
+      checked(a[14], at::kFloat, d.total_kv, "into_weight");
+      slots_to = d.total_kv;
+    }
+    on_current_device(a, {0, 1, 2, 3, 4, 5, 6, 7, 9, 10, 11, 12, 13, 14, 15});
+    Workspace w;
+    use_workspace(w, a[15], s, CP_WS_EVICT, k);
+    return status(call(cache_fn.evict, &s, pointer(k), pointer(a[1]), (int32_t*)pointer(a[2]),
+                       (float*)pointer(weight), (int32_t*)pointer(a[3]), (int32_t*)pointer(a[4]), budget,
+                       protect, (int32_t)sinks, pointer(a[9]), pointer(a[10]), (int32_t*)pointer(a[11]),
+                       (float*)pointer(a[14]), (int32_t*)pointer(a[12]), (int32_t*)pointer(a[13]),
+                       slots_to, w.ptr, w.bytes, stream_of(a[16])));
+  });
+}
+
 // which driver, address of a cp_ring_desc, stream
 PyObject* ring(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
@@ -354,8 +550,34 @@ PyObject* connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
   Py_RETURN_NONE;
 }
 
+// addresses of cp_tree_attn, cp_tree_accept, cp_kv_attn_weight, cp_kv_evict
+PyObject* connect_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 4) {
+    PyErr_SetString(PyExc_TypeError, "wrong number of arguments");
+    return nullptr;
+  }
+  void* p[4];
+  for (int i = 0; i < 4; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (p[i] == nullptr) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a function is missing");
+      return nullptr;
+    }
+  }
+  cache_fn.tree_attn = (decltype(cache_fn.tree_attn))p[0];
+  cache_fn.tree_accept = (decltype(cache_fn.tree_accept))p[1];
+  cache_fn.weight = (decltype(cache_fn.weight))p[2];
+  cache_fn.evict = (decltype(cache_fn.evict))p[3];
+  Py_RETURN_NONE;
+}
+
 PyMethodDef methods[] = {
     {"connect", (PyCFunction)(void*)connect, METH_FASTCALL, nullptr},
+    {"connect_cache", (PyCFunction)(void*)connect_cache, METH_FASTCALL, nullptr},
+    {"tree_attn", (PyCFunction)(void*)tree_attn, METH_FASTCALL, nullptr},
+    {"tree_accept", (PyCFunction)(void*)tree_accept, METH_FASTCALL, nullptr},
+    {"kv_weight", (PyCFunction)(void*)kv_weight, METH_FASTCALL, nullptr},
+    {"kv_evict", (PyCFunction)(void*)kv_evict, METH_FASTCALL, nullptr},
     {"partial", (PyCFunction)(void*)partial, METH_FASTCALL, nullptr},
     {"decode", (PyCFunction)(void*)decode, METH_FASTCALL, nullptr},
     {"decode_static", (PyCFunction)(void*)decode_static, METH_FASTCALL, nullptr},
