@@ -7,10 +7,11 @@
 // destinations in front of it: no row is read after it was written). The order of the slots means
 // nothing to attention, which goes by their positions.
 //
-// Two launches. The first, a workgroup per sequence, finds the weight of the last slot that stays by a
-// radix selection over order-preserving 32-bit keys (three digits of 11, 11 and 10 bits, counted in
-// LDS), then ranks holes and movers by prefix sums, and does the bookkeeping arrays. The second
-// copies the K and V rows.
+// The weight of the last slot that stays is found by a radix selection over order-preserving 32-bit
+// keys (three digits of 11, 11 and 10 bits); then ties, holes and movers are ranked by prefix sums
+// over 64-slot ballots. Sequences that one workgroup reads quickly are one launch, a workgroup
+// each, with the keys in LDS; longer ones are cut into chunks and take a launch per digit. The last
+// launch moves the rows and does the bookkeeping.
 #include "cp_common.h"
 
 namespace cp {
@@ -36,10 +37,16 @@ struct EvictParams {
   int64_t slots, slots_to;
   int32_t batch, sinks, chunks;
   bool in_place;
-  // workspace: what is copied where, [slots] at the sequence's first slot; and how many
-  int32_t* from;    // destination slot -> source slot, both within the sequence (in place: of move t)
-  int32_t* to;      // in place: destination slot of move t
-  int32_t* count;   // [batch]
+  // workspace, [slots] each, at the sequence's first slot
+  int32_t* to;      // in place: destination slot of move t; else, per slot that is filled, its source
+                    // slot, or -1 - t where move t fills it
+  int32_t* from;    // of move t: source slot, its position and weight
+  int32_t* from_pos;
+  float* from_weight;
+  int32_t* count;   // [batch][3]: slots that stay, moves, slots held before
+  // of sequences in chunks
+  int32_t* hist;    // [batch][HIST]
+  int32_t* chunk;   // [chunk][4]: slots above the bar, at it; the same in front of `keep`
 };
 
 __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
@@ -57,6 +64,8 @@ __device__ __forceinline__ Range range_of(const int32_t* cu, int b, int64_t slot
 
 constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64;
 constexpr int BINS = 2048;
+constexpr int CHUNK = 8192;               // slots of a chunk
+constexpr int HIST = 3 * BINS + 64;       // three digits' counts, and the number of protected slots
 
 // Order-preserving key of a weight; protected slots are above all, NaN below all.
 __device__ __forceinline__ uint32_t key_of(float w, bool safe) {
@@ -89,171 +98,459 @@ __device__ __forceinline__ int block_scan(int x, int* wave_sums, int* total) {
   return before + end - x;
 }
 
-__global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictParams p) {
-  __shared__ int hist[BINS];
-  __shared__ int wave_sums[SEL_WAVES];
-  __shared__ int found_bin, found_above;
-  const int b = blockIdx.x, tid = threadIdx.x;
-  const Range src = range_of(p.cu, b, p.slots), dst = range_of(p.cu_to, b, p.slots_to);
-  const int n = (int)clamp64(p.used[b], 0, src.room);
-  const int32_t from_pos = p.protect_from != nullptr ? p.protect_from[b] : CP_POS_PAD_KV;
-  const int32_t* const pos = p.kv_pos + src.first;
-  const float* const weight = p.weight + src.first;
-  auto key = [&](int i) -> uint32_t {
+// What a sequence keeps, and its slots' keys.
+struct EvictSeq {
+  Range src, dst;
+  int n;
+  int32_t sinks, from_pos;
+  const int32_t* pos;
+  const float* weight;
+  __device__ __forceinline__ EvictSeq(const EvictParams& p, int b) {
+    src = range_of(p.cu, b, p.slots);
+    dst = range_of(p.cu_to, b, p.slots_to);
+    n = (int)clamp64(p.used[b], 0, src.room);
+    sinks = p.sinks;
+    from_pos = p.protect_from != nullptr ? p.protect_from[b] : CP_POS_PAD_KV;
+    pos = p.kv_pos + src.first;
+    weight = p.weight + src.first;
+  }
+  __device__ __forceinline__ uint32_t key(int i) const {
     const int32_t at = pos[i];
     // (a padded token can be seen by no query: nothing protects it)
-    return key_of(weight[i], at != CP_POS_PAD_KV && (at < p.sinks || at >= from_pos));
-  };
-  int protected_n = 0;
-  for (int i = tid; i < n; i += SEL_THREADS) protected_n += key(i) == 0xffffffffu;
+    return key_of(weight[i], at != CP_POS_PAD_KV && (at < sinks || at >= from_pos));
+  }
+  __device__ __forceinline__ int keep(int64_t budget, int protected_n) const {
+    if (budget < protected_n) budget = protected_n;
+    return (int)clamp64(budget, 0, n < dst.room ? n : dst.room);
+  }
+};
+
+// The digit at which `left` slots, counted from the largest, are reached: c1 and c0 are the counts of
+// this thread's bins BINS-1-2t and BINS-2-2t. What lies above it is taken off `left`. (Uniform; two words of
+// LDS, free again after the next barrier.)
+__device__ __forceinline__ int find_digit(int c1, int c0, int& left, int* wave_sums, int* found) {
   int all;
-  block_scan(protected_n, wave_sums, &all);
-  int64_t want = p.budget[b];
-  if (want < all) want = all;
-  const int keep = (int)clamp64(want, 0, n < dst.room ? n : dst.room);
-
-  // the key of the last slot that stays, and how many slots with that key do
-  uint32_t bar = 0;
-  int ties = 0;
-  if (keep > 0 && keep < n) {
-    uint32_t prefix = 0, prefix_mask = 0;
-    int left = keep;
-    for (int d = 0; d < 3; ++d) {
-      const int shift = d == 0 ? 21 : d == 1 ? 10 : 0;
-      const uint32_t digit = d == 2 ? 1023u : 2047u;
-      __syncthreads();
-      for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
-      __syncthreads();
-      for (int i = tid; i < n; i += SEL_THREADS) {
-        const uint32_t x = key(i);
-        if ((x & prefix_mask) == prefix) atomicAdd(&hist[(x >> shift) & digit], 1);
-      }
-      __syncthreads();
-      // bins from the top: thread t has bins BINS-1-2t and BINS-2-2t
-      const int hi = BINS - 1 - 2 * tid;
-      const int c1 = hist[hi], c0 = hist[hi - 1];
-      const int above = block_scan(c0 + c1, wave_sums, &all);
-      if (above < left && left <= above + c1) {
-        found_bin = hi;
-        found_above = above;
-      } else if (above + c1 < left && left <= above + c1 + c0) {
-        found_bin = hi - 1;
-        found_above = above + c1;
-      }
-      __syncthreads();
-      prefix |= (uint32_t)found_bin << shift;
-      prefix_mask |= digit << shift;
-      left -= found_above;
-    }
-    bar = prefix;
-    ties = left;
+  const int above = block_scan(c0 + c1, wave_sums, &all);
+  const int hi = BINS - 1 - 2 * (int)threadIdx.x;
+  if (above < left && left <= above + c1) {
+    found[0] = hi;
+    found[1] = above;
+  } else if (above + c1 < left && left <= above + c1 + c0) {
+    found[0] = hi - 1;
+    found[1] = above + c1;
   }
-
-  // ranks of the holes in front of `keep` and of the movers behind it
-  int32_t* const from = p.from + src.first;
-  int32_t* const to = p.to + src.first;
-  int tie_base = 0, hole_base = 0, mover_base = 0;
-  for (int i0 = 0; i0 < n; i0 += SEL_THREADS) {
-    const int i = i0 + tid;
-    bool stays = false, tie = false;
-    if (i < n) {
-      if (keep == n) stays = true;
-      else if (keep > 0) {
-        const uint32_t x = key(i);
-        stays = x > bar;
-        tie = x == bar;
-      }
-    }
-    const int rank = block_scan(tie ? 1 : 0, wave_sums, &all);
-    if (tie && tie_base + rank < ties) stays = true;
-    tie_base += all;
-    const bool hole = i < keep && !stays, mover = i >= keep && i < n && stays;
-    // (holes lie in front of movers: one scan serves both)
-    const int r = block_scan((hole ? 1 : 0) | (mover ? 1 << 16 : 0), wave_sums, &all);
-    if (hole) to[hole_base + (r & 0xffff)] = i;
-    if (mover) from[mover_base + (r >> 16)] = i;
-    hole_base += all & 0xffff;
-    mover_base += all >> 16;
-  }
-  __threadfence_block();
   __syncthreads();
-  const int moves = hole_base;
-  if (p.in_place) {
-    for (int t = tid; t < moves; t += SEL_THREADS) {
-      const int d = to[t], s = from[t];
-      p.kv_pos[src.first + d] = pos[s];
-      p.weight[src.first + d] = weight[s];
+  left -= found[1];
+  return found[0];
+}
+__device__ constexpr int digit_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
+__device__ constexpr uint32_t digit_mask(int d) { return d == 2 ? 1023u : 2047u; }
+
+// Ranks of the slots [i0, i1) of a sequence among its ties, holes and movers, given those before i0:
+// the moves are listed. A wavefront's own, contiguous part; i0 a multiple of 64.
+struct Ranks {
+  int ties, holes, movers;
+};
+template <typename Key>
+__device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq& sq, int i0, int i1, int keep,
+                                           uint32_t bar, int ties, Ranks r, Key key) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t below = (1ull << lane) - 1;
+  for (int g = i0; g < i1; g += 64) {
+    const int i = g + lane;
+    const bool in = i < i1;
+    const uint32_t x = in ? key(i) : 0;
+    const bool tie = in && keep < sq.n && x == bar;
+    const uint64_t tied = __builtin_amdgcn_ballot_w64(tie);
+    bool stays = in && keep > 0 && (keep == sq.n || x > bar ||
+                                    (tie && r.ties + __builtin_popcountll(tied & below) < ties));
+    r.ties += __builtin_popcountll(tied);
+    const bool hole = in && i < keep && !stays, mover = in && i >= keep && stays;
+    const uint64_t holes = __builtin_amdgcn_ballot_w64(hole), movers = __builtin_amdgcn_ballot_w64(mover);
+    if (hole) {
+      const int t = r.holes + __builtin_popcountll(holes & below);
+      if (p.in_place) p.to[sq.src.first + t] = i;
+      else p.to[sq.src.first + i] = -1 - t;
+    } else if (!p.in_place && in && i < keep) {
+      p.to[sq.src.first + i] = i;
     }
-    __syncthreads();
-    for (int i = keep + tid; i < n; i += SEL_THREADS) {
-      p.kv_pos[src.first + i] = CP_POS_PAD_KV;
-      p.weight[src.first + i] = 0.f;
+    if (mover) {
+      const int64_t t = sq.src.first + r.movers + __builtin_popcountll(movers & below);
+      p.from[t] = i;
+      p.from_pos[t] = sq.pos[i];
+      p.from_weight[t] = sq.weight[i];
     }
-  } else {
-    for (int i = tid; i < keep; i += SEL_THREADS) {
-      p.pos_to[dst.first + i] = pos[i];
-      p.weight_to[dst.first + i] = weight[i];
-    }
-    for (int64_t i = keep + tid; i < dst.room; i += SEL_THREADS) {
-      p.pos_to[dst.first + i] = CP_POS_PAD_KV;
-      p.weight_to[dst.first + i] = 0.f;
-    }
-    __syncthreads();
-    for (int t = tid; t < moves; t += SEL_THREADS) {
-      const int d = to[t], s = from[t];
-      p.pos_to[dst.first + d] = pos[s];
-      p.weight_to[dst.first + d] = weight[s];
-    }
-  }
-  if (tid == 0) {
-    p.used_to[b] = keep;
-    p.count[2 * b] = keep;
-    p.count[2 * b + 1] = moves;
+    r.holes += __builtin_popcountll(holes);
+    r.movers += __builtin_popcountll(movers);
   }
 }
 
-// Rows of K and V: in place the moves, otherwise first what stays in its slot and then the moves.
+// A workgroup per sequence. The keys of the first `cached` slots are kept in LDS.
+__global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictParams p, int cached) {
+  extern __shared__ __align__(16) uint32_t keys[];
+  __shared__ int hist[BINS];
+  __shared__ int wave_sums[SEL_WAVES];
+  __shared__ int found[2];
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const EvictSeq sq(p, b);
+  const int64_t budget = p.budget[b];
+  for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
+  __syncthreads();
+  int protected_n = 0;
+  for (int i = tid; i < sq.n; i += SEL_THREADS) {
+    const uint32_t x = sq.key(i);
+    if (i < cached) keys[i] = x;
+    protected_n += x == 0xffffffffu;
+    atomicAdd(&hist[x >> digit_shift(0)], 1);
+  }
+  int all;
+  block_scan(protected_n, wave_sums, &all);   // (and the counts are complete)
+  const int keep = sq.keep(budget, all);
+  auto key = [&](int i) -> uint32_t { return i < cached ? keys[i] : sq.key(i); };
+
+  // the key of the last slot that stays, and how many slots with that key do
+  uint32_t bar = 0;
+  int ties = keep;
+  if (keep > 0 && keep < sq.n) {
+#pragma unroll
+    for (int d = 0; d < 3; ++d) {
+      if (d > 0) {
+        __syncthreads();
+        for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
+        __syncthreads();
+        const int above = digit_shift(d - 1);
+        for (int i = tid; i < sq.n; i += SEL_THREADS) {
+          const uint32_t x = key(i);
+          if (((x ^ bar) >> above) == 0) atomicAdd(&hist[(x >> digit_shift(d)) & digit_mask(d)], 1);
+        }
+        __syncthreads();
+      }
+      const int hi = BINS - 1 - 2 * tid;
+      bar |= (uint32_t)find_digit(hist[hi], hist[hi - 1], ties, wave_sums, found) << digit_shift(d);
+    }
+  }
+  if (keep < sq.n) {
+    // a contiguous part per wavefront: first how many of its slots lie above and at the bar, ...
+    const int part = ((sq.n + SEL_THREADS - 1) / SEL_THREADS) * 64;
+    const int i0 = min(sq.n, wave * part), i1 = min(sq.n, i0 + part);
+    int above = 0, tied = 0, front_above = 0, front_tied = 0;
+    for (int g = i0; g < i1; g += 64) {
+      const int i = g + lane;
+      const uint32_t x = i < i1 ? key(i) : 0;
+      const uint64_t up = __builtin_amdgcn_ballot_w64(i < i1 && keep > 0 && x > bar);
+      const uint64_t at = __builtin_amdgcn_ballot_w64(i < i1 && x == bar);
+      const uint64_t front = g >= keep ? 0 : keep - g >= 64 ? ~0ull : (1ull << (keep - g)) - 1;
+      above += __builtin_popcountll(up);
+      tied += __builtin_popcountll(at);
+      front_above += __builtin_popcountll(up & front);
+      front_tied += __builtin_popcountll(at & front);
+    }
+    __shared__ int counts[SEL_WAVES][4];
+    __syncthreads();
+    if (lane == 0) {
+      counts[wave][0] = above; counts[wave][1] = tied;
+      counts[wave][2] = front_above; counts[wave][3] = front_tied;
+    }
+    __syncthreads();
+    // ... then their ranks
+    Ranks r = {0, 0, 0};
+    for (int w = 0; w < wave; ++w) {
+      const int w0 = min(sq.n, w * part), size = min(keep, min(sq.n, w0 + part)) - min(keep, w0);
+      const int left = max(0, ties - r.ties);
+      const int front = counts[w][2] + min(left, counts[w][3]);
+      r.holes += size - front;
+      r.movers += counts[w][0] + min(left, counts[w][1]) - front;
+      r.ties += counts[w][1];
+    }
+    list_moves(p, sq, i0, i1, keep, bar, ties, r, key);
+    if (wave == SEL_WAVES - 1 && lane == 0) {
+      const int left = max(0, ties - r.ties);
+      const int size = min(keep, i1) - min(keep, i0);
+      p.count[3 * b + 1] = r.holes + size - (front_above + min(left, front_tied));
+    }
+  } else {
+    if (!p.in_place)
+      for (int i = tid; i < keep; i += SEL_THREADS) p.to[sq.src.first + i] = i;
+    if (tid == 0) p.count[3 * b + 1] = 0;
+  }
+  if (tid == 0) {
+    p.count[3 * b] = keep;
+    p.count[3 * b + 2] = sq.n;
+  }
+}
+
+// ---- sequences in chunks, a workgroup each ----
+
+// The sequence that chunk x of all sequences belongs to, and its first chunk.
+__device__ __forceinline__ int find_chunk(const EvictParams& p, int x, int* begin) {
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 64) {
+    int c = 0;
+    if (b0 + lane < p.batch) {
+      const int64_t room = range_of(p.cu, b0 + lane, p.slots).room;
+      c = (int)((clamp64(p.used[b0 + lane], 0, room) + CHUNK - 1) / CHUNK);
+    }
+    int end = c;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(end, o, 64);
+      if (lane >= o) end += y;
+    }
+    const uint64_t behind = __builtin_amdgcn_ballot_w64(base + end > x);
+    if (behind != 0) {
+      const int l = __builtin_ctzll(behind);
+      *begin = base + __shfl(end - c, l, 64);
+      return b0 + l;
+    }
+    base += __shfl(end, 63, 64);
+  }
+  return -1;
+}
+
+__global__ __launch_bounds__(256) void evict_clear_kernel(const EvictParams p) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < (int64_t)p.batch * HIST) p.hist[i] = 0;
+  if (i < (int64_t)p.batch * 3) p.count[i] = 0;   // (a sequence that holds nothing has no chunk)
+}
+
+// The bar as far as the digits before STEP tell it, and the slots with those digits that stay.
+struct Bar {
+  uint32_t value;
+  int keep, ties;
+};
+template <int STEP>
+__device__ __forceinline__ Bar bar_of(const EvictParams& p, const EvictSeq& sq, int b, int* wave_sums,
+                                      int* found) {
+  const int32_t* const h = p.hist + (int64_t)b * HIST;
+  Bar r;
+  r.value = 0;
+  r.keep = r.ties = sq.keep(p.budget[b], h[3 * BINS]);
+  if (r.keep == 0 || r.keep == sq.n) return r;   // uniform
+#pragma unroll
+  for (int d = 0; d < STEP; ++d) {
+    const int hi = BINS - 1 - 2 * (int)threadIdx.x;
+    r.value |= (uint32_t)find_digit(h[d * BINS + hi], h[d * BINS + hi - 1], r.ties, wave_sums, found)
+               << digit_shift(d);
+    __syncthreads();
+  }
+  return r;
+}
+
+// Counts of digit D among the slots that share the bar's digits before it.
+template <int D>
+__global__ __launch_bounds__(SEL_THREADS) void evict_digit_kernel(const EvictParams p) {
+  __shared__ int hist[BINS];
+  __shared__ int wave_sums[SEL_WAVES];
+  __shared__ int found[2];
+  int begin = 0;
+  const int b = find_chunk(p, blockIdx.x, &begin), tid = threadIdx.x;
+  if (b < 0) return;
+  const EvictSeq sq(p, b);
+  for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
+  __syncthreads();
+  const int i0 = ((int)blockIdx.x - begin) * CHUNK, i1 = min(sq.n, i0 + CHUNK);
+  int32_t* const h = p.hist + (int64_t)b * HIST;
+  Bar bar = {0, 0, 0};
+  if (D > 0) {
+    bar = bar_of<D>(p, sq, b, wave_sums, found);
+    if (bar.keep == 0 || bar.keep == sq.n) return;
+  }
+  int protected_n = 0;
+  for (int i = i0 + tid; i < i1; i += SEL_THREADS) {
+    const uint32_t x = sq.key(i);
+    if (D == 0) protected_n += x == 0xffffffffu;
+    if (D == 0 || ((x ^ bar.value) >> digit_shift(D > 0 ? D - 1 : 0)) == 0)
+      atomicAdd(&hist[(x >> digit_shift(D)) & digit_mask(D)], 1);
+  }
+  int all;
+  block_scan(protected_n, wave_sums, &all);   // (and the counts are complete)
+  if (D == 0 && tid == 0 && all > 0) atomicAdd(&h[3 * BINS], all);
+  for (int i = tid; i < BINS; i += SEL_THREADS)
+    if (hist[i] != 0) atomicAdd(&h[D * BINS + i], hist[i]);
+}
+
+__global__ __launch_bounds__(SEL_THREADS) void evict_count_kernel(const EvictParams p) {
+  __shared__ int wave_sums[SEL_WAVES];
+  __shared__ int found[2];
+  __shared__ int counts[4];
+  int begin = 0;
+  const int b = find_chunk(p, blockIdx.x, &begin), tid = threadIdx.x;
+  if (b < 0) return;
+  const EvictSeq sq(p, b);
+  if (tid < 4) counts[tid] = 0;
+  const Bar bar = bar_of<3>(p, sq, b, wave_sums, found);
+  __syncthreads();
+  const int i0 = ((int)blockIdx.x - begin) * CHUNK, i1 = min(sq.n, i0 + CHUNK);
+  int c[4] = {0, 0, 0, 0};
+  for (int i = i0 + tid; i < i1; i += SEL_THREADS) {
+    const uint32_t x = sq.key(i);
+    const bool up = bar.keep > 0 && x > bar.value, at = x == bar.value;
+    c[0] += up;
+    c[1] += at;
+    c[2] += up && i < bar.keep;
+    c[3] += at && i < bar.keep;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) c[k] += __shfl_xor(c[k], o, 64);
+    if ((tid & 63) == 0) atomicAdd(&counts[k], c[k]);
+  }
+  __syncthreads();
+  if (tid < 4) p.chunk[(int64_t)blockIdx.x * 4 + tid] = counts[tid];
+}
+
+__global__ __launch_bounds__(SEL_THREADS) void evict_list_kernel(const EvictParams p) {
+  __shared__ int wave_sums[SEL_WAVES];
+  __shared__ int found[2];
+  __shared__ int counts[SEL_WAVES][4];
+  int begin = 0;
+  const int b = find_chunk(p, blockIdx.x, &begin), tid = threadIdx.x;
+  if (b < 0) return;
+  const int lane = tid & 63, wave = tid >> 6;
+  const EvictSeq sq(p, b);
+  const Bar bar = bar_of<3>(p, sq, b, wave_sums, found);
+  const int keep = bar.keep, ties = bar.ties;
+  const int i0 = ((int)blockIdx.x - begin) * CHUNK, i1 = min(sq.n, i0 + CHUNK);
+  constexpr int PART = CHUNK / SEL_WAVES, PER = PART / 64;
+  const int p0 = min(i1, i0 + wave * PART), p1 = min(i1, p0 + PART);
+  uint32_t x[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int i = p0 + k * 64 + lane;
+    x[k] = i < p1 ? sq.key(i) : 0;
+  }
+  int c[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int i = p0 + k * 64 + lane;
+    const uint64_t up = __builtin_amdgcn_ballot_w64(i < p1 && keep > 0 && x[k] > bar.value);
+    const uint64_t at = __builtin_amdgcn_ballot_w64(i < p1 && x[k] == bar.value);
+    const int left = keep - (p0 + k * 64);
+    const uint64_t front = left <= 0 ? 0 : left >= 64 ? ~0ull : (1ull << left) - 1;
+    c[0] += __builtin_popcountll(up);
+    c[1] += __builtin_popcountll(at);
+    c[2] += __builtin_popcountll(up & front);
+    c[3] += __builtin_popcountll(at & front);
+  }
+  if (lane == 0)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) counts[wave][k] = c[k];
+  __syncthreads();
+  Ranks r = {0, 0, 0};
+  auto pass = [&](const int* n4, int first, int last) {   // the slots [first, last) and their counts
+    if (keep == sq.n) return;
+    const int left = max(0, ties - r.ties);
+    const int front = n4[2] + min(left, n4[3]);
+    r.holes += min(keep, last) - min(keep, first) - front;
+    r.movers += n4[0] + min(left, n4[1]) - front;
+    r.ties += n4[1];
+  };
+  if (keep < sq.n) {   // the chunks before, a lane each
+    for (int k0 = begin; k0 < (int)blockIdx.x; k0 += 64) {
+      const int k = k0 + lane;
+      const bool in = k < (int)blockIdx.x;
+      const int4 y = in ? *(const int4*)(p.chunk + (int64_t)k * 4) : make_int4(0, 0, 0, 0);
+      int end = y.y;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int z = __shfl_up(end, o, 64);
+        if (lane >= o) end += z;
+      }
+      const int left = max(0, ties - (r.ties + end - y.y));
+      const int front = y.z + min(left, y.w);
+      const int size = min(keep, (k - begin + 1) * CHUNK) - min(keep, (k - begin) * CHUNK);
+      int holes = in ? size - front : 0, movers = in ? y.x + min(left, y.y) - front : 0;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        holes += __shfl_xor(holes, o, 64);
+        movers += __shfl_xor(movers, o, 64);
+      }
+      r.holes += holes;
+      r.movers += movers;
+      r.ties += __shfl(end, 63, 64);
+    }
+  }
+  for (int w = 0; w < wave; ++w)
+    pass(counts[w], min(i1, i0 + w * PART), min(i1, i0 + (w + 1) * PART));
+  if (keep < sq.n || !p.in_place) list_moves(p, sq, p0, p1, keep, bar.value, ties, r, [&](int i) { return sq.key(i); });
+  if (i1 == sq.n && wave == SEL_WAVES - 1) {
+    pass(counts[wave], p0, p1);
+    if (lane == 0) {
+      p.count[3 * b] = keep;
+      p.count[3 * b + 1] = r.holes;
+      p.count[3 * b + 2] = sq.n;
+    }
+  }
+}
+
+// Rows and bookkeeping: in place the moves, otherwise all slots that are filled; and what is behind.
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
   const int b = blockIdx.y;
-  const Range src = range_of(p.cu, b, p.slots), dst = range_of(p.cu_to, b, p.slots_to);
-  const int keep = p.count[2 * b], moves = p.count[2 * b + 1];
-  const int32_t* const from = p.from + src.first;
-  const int32_t* const to = p.to + src.first;
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  const int64_t first = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (p.in_place) {
-    for (int64_t e = first; e < (int64_t)moves * p.chunks; e += stride) {
-      const int64_t t = e / p.chunks, c = e - t * p.chunks;
-      const int64_t s = (src.first + from[t]) * p.chunks + c, d = (dst.first + to[t]) * p.chunks + c;
-      p.k_to[d] = p.k[s];
-      p.v_to[d] = p.v[s];
+  const Range from = range_of(p.cu, b, p.slots), to = range_of(p.cu_to, b, p.slots_to);
+  // (`used` is written below, and in place it is the one that was read: the count before is listed)
+  const int keep = p.count[3 * b], moves = p.count[3 * b + 1], n = p.count[3 * b + 2];
+  const int64_t s0 = from.first, d0 = to.first;
+  const int stride = gridDim.x * 256, first = blockIdx.x * 256 + threadIdx.x;
+  const int rows = p.in_place ? moves : keep;
+  for (int64_t e = first; e < (int64_t)rows * p.chunks; e += stride) {
+    const int i = (int)(e / p.chunks), c = (int)(e - (int64_t)i * p.chunks);
+    int s, d;
+    if (p.in_place) {
+      s = p.from[s0 + i];
+      d = p.to[s0 + i];
+    } else {
+      const int m = p.to[s0 + i];
+      s = m >= 0 ? m : p.from[s0 - 1 - m];
+      d = i;
     }
-    return;
-  }
-  for (int64_t e = first; e < (int64_t)keep * p.chunks; e += stride) {
-    const int64_t i = e / p.chunks, c = e - i * p.chunks;
-    // is slot i a hole? `to` is ascending
-    int lo = 0, hi = moves;
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (to[mid] < i) lo = mid + 1;
-      else hi = mid;
+    const int64_t src = (s0 + s) * p.chunks + c, dst = (d0 + d) * p.chunks + c;
+    const uint4 k = p.k[src], v = p.v[src];
+    p.k_to[dst] = k;
+    p.v_to[dst] = v;
+    if (c == 0) {
+      // (in place the movers' own entries may be cleared already: theirs were listed)
+      const int t = p.in_place ? i : -1 - p.to[s0 + i];
+      p.pos_to[d0 + d] = t >= 0 ? p.from_pos[s0 + t] : p.kv_pos[s0 + s];
+      p.weight_to[d0 + d] = t >= 0 ? p.from_weight[s0 + t] : p.weight[s0 + s];
     }
-    const int64_t s0 = lo < moves && to[lo] == i ? from[lo] : i;
-    const int64_t s = (src.first + s0) * p.chunks + c, d = (dst.first + i) * p.chunks + c;
-    p.k_to[d] = p.k[s];
-    p.v_to[d] = p.v[s];
   }
+  const int64_t end = p.in_place ? n : to.room;
+  for (int64_t i = keep + first; i < end; i += stride) {
+    p.pos_to[d0 + i] = CP_POS_PAD_KV;
+    p.weight_to[d0 + i] = 0.f;
+  }
+  if (first == 0) p.used_to[b] = keep;
 }
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Above this many slots a sequence, on average, they are cut into chunks.
+constexpr int64_t kChunkedSlots = 32768;
+constexpr int kCachedKeys = 32768;   // keys in LDS at most: 128 KB
+
+struct EvictPlan {
+  bool chunked;
+  int64_t chunks;   // there can be
+  size_t list, count, hist, chunk, bytes;
+};
+EvictPlan evict_plan(const cp_shape& s) {
+  EvictPlan pl = {};
+  pl.chunked = s.total_kv / s.batch > kChunkedSlots;
+  pl.chunks = s.total_kv / CHUNK + s.batch;
+  pl.list = round256((size_t)s.total_kv * 4);
+  pl.count = round256((size_t)s.batch * 12);
+  pl.hist = pl.chunked ? round256((size_t)s.batch * HIST * 4) : 0;
+  pl.chunk = pl.chunked ? round256((size_t)pl.chunks * 16) : 0;
+  pl.bytes = 4 * pl.list + pl.count + pl.hist + pl.chunk;
+  return pl;
+}
+
 }  // namespace
 
-size_t evict_workspace_bytes(const cp_shape& s) {
-  return 2 * round256((size_t)s.total_kv * 4) + round256((size_t)s.batch * 8);
-}
+size_t evict_workspace_bytes(const cp_shape& s) { return evict_plan(s).bytes; }
 
 }  // namespace cp
 
@@ -291,8 +588,8 @@ extern "C" int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, 
   if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(k_to) || !aligned16(v_to))
     return CP_ERR_ALIGN;
   if (s.batch > 65535) return CP_ERR_SHAPE;   // the grid's second dimension
-  if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 ||
-      workspace_bytes < evict_workspace_bytes(s))
+  const EvictPlan pl = evict_plan(s);
+  if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 || workspace_bytes < pl.bytes)
     return CP_ERR_WORKSPACE;
   EvictParams p = {};
   p.k = (const uint4*)k_cache; p.v = (const uint4*)v_cache; p.kv_pos = kv_pos_cache; p.weight = weight;
@@ -304,12 +601,39 @@ extern "C" int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, 
   p.batch = s.batch; p.sinks = sinks;
   p.chunks = (int32_t)((int64_t)s.n_kv_heads * s.head_dim * (s.dtype == CP_BF16 ? 2 : 4) / 16);
   p.in_place = in_place;
-  char* const ws = (char*)workspace;
-  p.from = (int32_t*)ws;
-  p.to = (int32_t*)(ws + round256((size_t)s.total_kv * 4));
-  p.count = (int32_t*)(ws + 2 * round256((size_t)s.total_kv * 4));
+  char* ws = (char*)workspace;
+  auto take = [&ws](size_t bytes) {
+    char* const at = ws;
+    ws += bytes;
+    return at;
+  };
+  p.to = (int32_t*)take(pl.list);
+  p.from = (int32_t*)take(pl.list);
+  p.from_pos = (int32_t*)take(pl.list);
+  p.from_weight = (float*)take(pl.list);
+  p.count = (int32_t*)take(pl.count);
+  p.hist = (int32_t*)take(pl.hist);
+  p.chunk = (int32_t*)take(pl.chunk);
   hipStream_t st = (hipStream_t)stream;
-  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)s.batch), dim3(SEL_THREADS), 0, st, p);
+  if (pl.chunked) {
+    const dim3 grid((unsigned)pl.chunks), block(SEL_THREADS);
+    hipLaunchKernelGGL(evict_clear_kernel, dim3((unsigned)(((int64_t)s.batch * HIST + 255) / 256)), dim3(256),
+                       0, st, p);
+    hipLaunchKernelGGL(evict_digit_kernel<0>, grid, block, 0, st, p);
+    hipLaunchKernelGGL(evict_digit_kernel<1>, grid, block, 0, st, p);
+    hipLaunchKernelGGL(evict_digit_kernel<2>, grid, block, 0, st, p);
+    hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, st, p);
+    hipLaunchKernelGGL(evict_list_kernel, grid, block, 0, st, p);
+  } else {
+    // (a batch of more sequences than CUs: two workgroups share one)
+    const int64_t most = s.batch > 256 ? kCachedKeys / 4 : kCachedKeys;
+    const int cached = (int)(s.total_kv < most ? s.total_kv : most);
+    if (hipFuncSetAttribute((const void*)evict_select_kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                            kCachedKeys * 4) != hipSuccess)
+      return CP_ERR_LAUNCH;
+    hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)s.batch), dim3(SEL_THREADS), cached * 4, st, p,
+                       cached);
+  }
   if (check_launch() != CP_OK) return CP_ERR_LAUNCH;
   // enough workgroups for every CU, no more than there are chunks
   const int64_t rows = in_place ? s.total_kv : slots_to < s.total_kv ? slots_to : s.total_kv;

@@ -363,6 +363,8 @@ EVICTS = {     # lens, budgets, KV heads, head_dim, dtype
     "one_each": ([700, 1500, 40], [699, 1499, 39], 1, 128, "bf16"),
     "long": ([70000], [5000], 1, 64, "bf16"),
     "long_and_short": ([40000, 3], [39990, 2], 1, 64, "bf16"),
+    "chunks": ([90000, 0, 70000, 5, 8192], [50000, 0, 69999, 4, 8000], 1, 8, "bf16"),
+    "chunks_one_each": ([66000, 65537], [65999, 65536], 1, 8, "bf16"),
     "fp32": ([100, 50], [30, 49], 3, 24, "fp32"),
 }
 
