@@ -40,10 +40,8 @@ struct EvictParams {
   // workspace, [slots] each, at the sequence's first slot
   int32_t* to;      // in place: destination slot of move t; else, per slot that is filled, its source
                     // slot, or -1 - t where move t fills it
-  int32_t* from;    // of move t: source slot, its position and weight
-  int32_t* from_pos;
-  float* from_weight;
-  int32_t* count;   // [batch][3]: slots that stay, moves, slots held before
+  int32_t* from;    // source slot of move t
+  int32_t* count;   // [batch][2]: slots that stay, moves
   // of sequences in chunks
   int32_t* hist;    // [batch][HIST]
   int32_t* chunk;   // [chunk][4]: slots above the bar, at it; the same in front of `keep`
@@ -101,29 +99,55 @@ __device__ __forceinline__ int block_scan(int x, int* wave_sums, int* total) {
 // What a sequence keeps, and its slots' keys.
 struct EvictSeq {
   Range src, dst;
-  int n;
-  int32_t sinks, from_pos;
-  const int32_t* pos;
-  const float* weight;
+  int32_t n, from_pos, budget;
+  __device__ __forceinline__ EvictSeq() {}
   __device__ __forceinline__ EvictSeq(const EvictParams& p, int b) {
     src = range_of(p.cu, b, p.slots);
     dst = range_of(p.cu_to, b, p.slots_to);
     n = (int)clamp64(p.used[b], 0, src.room);
-    sinks = p.sinks;
     from_pos = p.protect_from != nullptr ? p.protect_from[b] : CP_POS_PAD_KV;
-    pos = p.kv_pos + src.first;
-    weight = p.weight + src.first;
+    budget = p.budget[b];
   }
-  __device__ __forceinline__ uint32_t key(int i) const {
-    const int32_t at = pos[i];
+  __device__ __forceinline__ EvictSeq of_lane(int l) const {
+    EvictSeq r;
+    r.src.first = __shfl(src.first, l, 64); r.src.room = __shfl(src.room, l, 64);
+    r.dst.first = __shfl(dst.first, l, 64); r.dst.room = __shfl(dst.room, l, 64);
+    r.n = __shfl(n, l, 64);
+    r.from_pos = __shfl(from_pos, l, 64);
+    r.budget = __shfl(budget, l, 64);
+    return r;
+  }
+  __device__ __forceinline__ uint32_t key(const EvictParams& p, int32_t at, float w) const {
     // (a padded token can be seen by no query: nothing protects it)
-    return key_of(weight[i], at != CP_POS_PAD_KV && (at < sinks || at >= from_pos));
+    return key_of(w, at != CP_POS_PAD_KV && (at < p.sinks || at >= from_pos));
   }
-  __device__ __forceinline__ int keep(int64_t budget, int protected_n) const {
-    if (budget < protected_n) budget = protected_n;
-    return (int)clamp64(budget, 0, n < dst.room ? n : dst.room);
+  __device__ __forceinline__ uint32_t key(const EvictParams& p, int i) const {
+    return key(p, p.kv_pos[src.first + i], p.weight[src.first + i]);
+  }
+  __device__ __forceinline__ int keep(int protected_n) const {
+    const int64_t want = budget < protected_n ? protected_n : budget;
+    return (int)clamp64(want, 0, n < dst.room ? n : dst.room);
   }
 };
+// The keys of the K slots i, i + step, ... that lie in front of `end`, all requested at once.
+template <int K>
+__device__ __forceinline__ void load_keys(const EvictParams& p, const EvictSeq& sq, int i, int step, int end,
+                                          uint32_t (&x)[K]) {
+  int32_t at[K];
+  float w[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int j = i + k * step;
+    at[k] = CP_POS_PAD_KV;
+    w[k] = 0.f;
+    if (j < end) {
+      at[k] = p.kv_pos[sq.src.first + j];
+      w[k] = p.weight[sq.src.first + j];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) x[k] = sq.key(p, at[k], w[k]);
+}
 
 // The digit at which `left` slots, counted from the largest, are reached: c1 and c0 are the counts of
 // this thread's bins BINS-1-2t and BINS-2-2t. What lies above it is taken off `left`. (Uniform; two words of
@@ -146,43 +170,49 @@ __device__ __forceinline__ int find_digit(int c1, int c0, int& left, int* wave_s
 __device__ constexpr int digit_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
 __device__ constexpr uint32_t digit_mask(int d) { return d == 2 ? 1023u : 2047u; }
 
-// Ranks of the slots [i0, i1) of a sequence among its ties, holes and movers, given those before i0:
-// the moves are listed. A wavefront's own, contiguous part; i0 a multiple of 64.
+// Of the slots of a sequence in front of some slot: ties with the bar, holes, movers.
 struct Ranks {
   int ties, holes, movers;
 };
-template <typename Key>
-__device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq& sq, int i0, int i1, int keep,
-                                           uint32_t bar, int ties, Ranks r, Key key) {
-  const int lane = threadIdx.x & 63;
+// The 64 slots from g on (`in`: there is one for this lane, with key x): moves are listed, and in
+// place the bookkeeping of what goes is cleared. (Keys are read by the wavefront that lists them.)
+__device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq& sq, int g, bool in, uint32_t x,
+                                           int keep, uint32_t bar, int ties, Ranks& r) {
+  const int lane = threadIdx.x & 63, i = g + lane;
   const uint64_t below = (1ull << lane) - 1;
-  for (int g = i0; g < i1; g += 64) {
-    const int i = g + lane;
-    const bool in = i < i1;
-    const uint32_t x = in ? key(i) : 0;
-    const bool tie = in && keep < sq.n && x == bar;
-    const uint64_t tied = __builtin_amdgcn_ballot_w64(tie);
-    bool stays = in && keep > 0 && (keep == sq.n || x > bar ||
-                                    (tie && r.ties + __builtin_popcountll(tied & below) < ties));
-    r.ties += __builtin_popcountll(tied);
-    const bool hole = in && i < keep && !stays, mover = in && i >= keep && stays;
-    const uint64_t holes = __builtin_amdgcn_ballot_w64(hole), movers = __builtin_amdgcn_ballot_w64(mover);
-    if (hole) {
-      const int t = r.holes + __builtin_popcountll(holes & below);
-      if (p.in_place) p.to[sq.src.first + t] = i;
-      else p.to[sq.src.first + i] = -1 - t;
-    } else if (!p.in_place && in && i < keep) {
-      p.to[sq.src.first + i] = i;
-    }
-    if (mover) {
-      const int64_t t = sq.src.first + r.movers + __builtin_popcountll(movers & below);
-      p.from[t] = i;
-      p.from_pos[t] = sq.pos[i];
-      p.from_weight[t] = sq.weight[i];
-    }
-    r.holes += __builtin_popcountll(holes);
-    r.movers += __builtin_popcountll(movers);
+  const bool tie = in && keep < sq.n && x == bar;
+  const uint64_t tied = __builtin_amdgcn_ballot_w64(tie);
+  const bool stays = in && keep > 0 && (keep == sq.n || x > bar ||
+                                        (tie && r.ties + __builtin_popcountll(tied & below) < ties));
+  r.ties += __builtin_popcountll(tied);
+  const bool hole = in && i < keep && !stays, mover = in && i >= keep && stays;
+  const uint64_t holes = __builtin_amdgcn_ballot_w64(hole), movers = __builtin_amdgcn_ballot_w64(mover);
+  if (hole) {
+    const int t = r.holes + __builtin_popcountll(holes & below);
+    if (p.in_place) p.to[sq.src.first + t] = i;
+    else p.to[sq.src.first + i] = -1 - t;
+  } else if (!p.in_place && in && i < keep) {
+    p.to[sq.src.first + i] = i;
   }
+  if (mover) p.from[sq.src.first + r.movers + __builtin_popcountll(movers & below)] = i;
+  if (p.in_place && in && i >= keep && !stays) {
+    p.kv_pos[sq.src.first + i] = CP_POS_PAD_KV;
+    p.weight[sq.src.first + i] = 0.f;
+  }
+  r.holes += __builtin_popcountll(holes);
+  r.movers += __builtin_popcountll(movers);
+}
+
+// Slots above the bar and at it among the 64 from g on, all of them and those in front of `keep`.
+__device__ __forceinline__ void count_slots(int g, bool in, uint32_t x, int keep, uint32_t bar, int (&c)[4]) {
+  const uint64_t up = __builtin_amdgcn_ballot_w64(in && keep > 0 && x > bar);
+  const uint64_t at = __builtin_amdgcn_ballot_w64(in && x == bar);
+  const int left = keep - g;
+  const uint64_t front = left <= 0 ? 0 : left >= 64 ? ~0ull : (1ull << left) - 1;
+  c[0] += __builtin_popcountll(up);
+  c[1] += __builtin_popcountll(at);
+  c[2] += __builtin_popcountll(up & front);
+  c[3] += __builtin_popcountll(at & front);
 }
 
 // A workgroup per sequence. The keys of the first `cached` slots are kept in LDS.
@@ -193,20 +223,26 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
   __shared__ int found[2];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const EvictSeq sq(p, b);
-  const int64_t budget = p.budget[b];
   for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
   __syncthreads();
   int protected_n = 0;
-  for (int i = tid; i < sq.n; i += SEL_THREADS) {
-    const uint32_t x = sq.key(i);
-    if (i < cached) keys[i] = x;
-    protected_n += x == 0xffffffffu;
-    atomicAdd(&hist[x >> digit_shift(0)], 1);
+  constexpr int AT_ONCE = 8;
+  for (int i0 = tid; i0 < sq.n; i0 += AT_ONCE * SEL_THREADS) {
+    uint32_t x[AT_ONCE];
+    load_keys(p, sq, i0, SEL_THREADS, sq.n, x);
+#pragma unroll
+    for (int k = 0; k < AT_ONCE; ++k) {
+      const int i = i0 + k * SEL_THREADS;
+      if (i >= sq.n) break;
+      if (i < cached) keys[i] = x[k];
+      protected_n += x[k] == 0xffffffffu;
+      atomicAdd(&hist[x[k] >> digit_shift(0)], 1);
+    }
   }
   int all;
   block_scan(protected_n, wave_sums, &all);   // (and the counts are complete)
-  const int keep = sq.keep(budget, all);
-  auto key = [&](int i) -> uint32_t { return i < cached ? keys[i] : sq.key(i); };
+  const int keep = sq.keep(all);
+  auto key = [&](int i) -> uint32_t { return i < cached ? keys[i] : sq.key(p, i); };
 
   // the key of the last slot that stays, and how many slots with that key do
   uint32_t bar = 0;
@@ -233,24 +269,15 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
     // a contiguous part per wavefront: first how many of its slots lie above and at the bar, ...
     const int part = ((sq.n + SEL_THREADS - 1) / SEL_THREADS) * 64;
     const int i0 = min(sq.n, wave * part), i1 = min(sq.n, i0 + part);
-    int above = 0, tied = 0, front_above = 0, front_tied = 0;
+    int c[4] = {0, 0, 0, 0};
     for (int g = i0; g < i1; g += 64) {
-      const int i = g + lane;
-      const uint32_t x = i < i1 ? key(i) : 0;
-      const uint64_t up = __builtin_amdgcn_ballot_w64(i < i1 && keep > 0 && x > bar);
-      const uint64_t at = __builtin_amdgcn_ballot_w64(i < i1 && x == bar);
-      const uint64_t front = g >= keep ? 0 : keep - g >= 64 ? ~0ull : (1ull << (keep - g)) - 1;
-      above += __builtin_popcountll(up);
-      tied += __builtin_popcountll(at);
-      front_above += __builtin_popcountll(up & front);
-      front_tied += __builtin_popcountll(at & front);
+      const bool in = g + lane < i1;
+      count_slots(g, in, in ? key(g + lane) : 0, keep, bar, c);
     }
     __shared__ int counts[SEL_WAVES][4];
-    __syncthreads();
-    if (lane == 0) {
-      counts[wave][0] = above; counts[wave][1] = tied;
-      counts[wave][2] = front_above; counts[wave][3] = front_tied;
-    }
+    if (lane == 0)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) counts[wave][k] = c[k];
     __syncthreads();
     // ... then their ranks
     Ranks r = {0, 0, 0};
@@ -262,35 +289,36 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
       r.movers += counts[w][0] + min(left, counts[w][1]) - front;
       r.ties += counts[w][1];
     }
-    list_moves(p, sq, i0, i1, keep, bar, ties, r, key);
+    const Ranks before = r;
+    for (int g = i0; g < i1; g += 64) {
+      const bool in = g + lane < i1;
+      list_moves(p, sq, g, in, in ? key(g + lane) : 0, keep, bar, ties, r);
+    }
+    r = before;
     if (wave == SEL_WAVES - 1 && lane == 0) {
       const int left = max(0, ties - r.ties);
       const int size = min(keep, i1) - min(keep, i0);
-      p.count[3 * b + 1] = r.holes + size - (front_above + min(left, front_tied));
+      p.count[2 * b + 1] = r.holes + size - (c[2] + min(left, c[3]));
     }
   } else {
     if (!p.in_place)
       for (int i = tid; i < keep; i += SEL_THREADS) p.to[sq.src.first + i] = i;
-    if (tid == 0) p.count[3 * b + 1] = 0;
+    if (tid == 0) p.count[2 * b + 1] = 0;
   }
-  if (tid == 0) {
-    p.count[3 * b] = keep;
-    p.count[3 * b + 2] = sq.n;
-  }
+  if (tid == 0) p.count[2 * b] = keep;
 }
 
 // ---- sequences in chunks, a workgroup each ----
 
-// The sequence that chunk x of all sequences belongs to, and its first chunk.
-__device__ __forceinline__ int find_chunk(const EvictParams& p, int x, int* begin) {
+// The sequence that chunk x of all sequences belongs to (its number, what it holds), and its first
+// chunk. Everything that a lane's sequence is described by is requested at once.
+__device__ __forceinline__ int find_chunk(const EvictParams& p, int x, int* begin, EvictSeq* sq) {
   const int lane = threadIdx.x & 63;
   int base = 0;
   for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    int c = 0;
-    if (b0 + lane < p.batch) {
-      const int64_t room = range_of(p.cu, b0 + lane, p.slots).room;
-      c = (int)((clamp64(p.used[b0 + lane], 0, room) + CHUNK - 1) / CHUNK);
-    }
+    const bool in = b0 + lane < p.batch;
+    const EvictSeq mine(p, in ? b0 + lane : b0);
+    const int c = in ? (mine.n + CHUNK - 1) / CHUNK : 0;
     int end = c;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -301,6 +329,7 @@ __device__ __forceinline__ int find_chunk(const EvictParams& p, int x, int* begi
     if (behind != 0) {
       const int l = __builtin_ctzll(behind);
       *begin = base + __shfl(end - c, l, 64);
+      *sq = mine.of_lane(l);
       return b0 + l;
     }
     base += __shfl(end, 63, 64);
@@ -311,31 +340,36 @@ __device__ __forceinline__ int find_chunk(const EvictParams& p, int x, int* begi
 __global__ __launch_bounds__(256) void evict_clear_kernel(const EvictParams p) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i < (int64_t)p.batch * HIST) p.hist[i] = 0;
-  if (i < (int64_t)p.batch * 3) p.count[i] = 0;   // (a sequence that holds nothing has no chunk)
+  if (i < (int64_t)p.batch * 2) p.count[i] = 0;   // (a sequence that holds nothing has no chunk)
 }
 
-// The bar as far as the digits before STEP tell it, and the slots with those digits that stay.
-struct Bar {
-  uint32_t value;
-  int keep, ties;
-};
+// The bar as far as the digits before STEP tell it, and the slots with those digits that stay. The
+// counts are requested by the constructor.
 template <int STEP>
-__device__ __forceinline__ Bar bar_of(const EvictParams& p, const EvictSeq& sq, int b, int* wave_sums,
-                                      int* found) {
-  const int32_t* const h = p.hist + (int64_t)b * HIST;
-  Bar r;
-  r.value = 0;
-  r.keep = r.ties = sq.keep(p.budget[b], h[3 * BINS]);
-  if (r.keep == 0 || r.keep == sq.n) return r;   // uniform
-#pragma unroll
-  for (int d = 0; d < STEP; ++d) {
+struct Bar {
+  int c1[STEP > 0 ? STEP : 1], c0[STEP > 0 ? STEP : 1], protected_n;
+  uint32_t value = 0;
+  int keep = 0, ties = 0;
+  __device__ __forceinline__ Bar(const EvictParams& p, int b) {
+    const int32_t* const h = p.hist + (int64_t)b * HIST;
     const int hi = BINS - 1 - 2 * (int)threadIdx.x;
-    r.value |= (uint32_t)find_digit(h[d * BINS + hi], h[d * BINS + hi - 1], r.ties, wave_sums, found)
-               << digit_shift(d);
-    __syncthreads();
+#pragma unroll
+    for (int d = 0; d < STEP; ++d) {
+      c1[d] = h[d * BINS + hi];
+      c0[d] = h[d * BINS + hi - 1];
+    }
+    protected_n = h[3 * BINS];
   }
-  return r;
-}
+  // (uniform)
+  __device__ __forceinline__ void find(const EvictSeq& sq, int* wave_sums, int* found) {
+    keep = ties = sq.keep(protected_n);
+    if (keep == 0 || keep == sq.n) return;
+#pragma unroll
+    for (int d = 0; d < STEP; ++d)
+      value |= (uint32_t)find_digit(c1[d], c0[d], ties, wave_sums, found) << digit_shift(d);
+  }
+};
+constexpr int PART = CHUNK / SEL_WAVES, PER = PART / 64;   // slots of a chunk's wavefront, of a lane
 
 // Counts of digit D among the slots that share the bar's digits before it.
 template <int D>
@@ -344,114 +378,87 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_digit_kernel(const EvictPar
   __shared__ int wave_sums[SEL_WAVES];
   __shared__ int found[2];
   int begin = 0;
-  const int b = find_chunk(p, blockIdx.x, &begin), tid = threadIdx.x;
+  EvictSeq sq;
+  const int b = find_chunk(p, blockIdx.x, &begin, &sq), tid = threadIdx.x;
   if (b < 0) return;
-  const EvictSeq sq(p, b);
-  for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
-  __syncthreads();
   const int i0 = ((int)blockIdx.x - begin) * CHUNK, i1 = min(sq.n, i0 + CHUNK);
-  int32_t* const h = p.hist + (int64_t)b * HIST;
-  Bar bar = {0, 0, 0};
+  Bar<D> bar(p, b);
+  uint32_t x[PER];
+  load_keys(p, sq, i0 + tid, SEL_THREADS, i1, x);
+  for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
   if (D > 0) {
-    bar = bar_of<D>(p, sq, b, wave_sums, found);
+    bar.find(sq, wave_sums, found);
     if (bar.keep == 0 || bar.keep == sq.n) return;
   }
+  __syncthreads();
   int protected_n = 0;
-  for (int i = i0 + tid; i < i1; i += SEL_THREADS) {
-    const uint32_t x = sq.key(i);
-    if (D == 0) protected_n += x == 0xffffffffu;
-    if (D == 0 || ((x ^ bar.value) >> digit_shift(D > 0 ? D - 1 : 0)) == 0)
-      atomicAdd(&hist[(x >> digit_shift(D)) & digit_mask(D)], 1);
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    if (i0 + tid + k * SEL_THREADS >= i1) break;
+    if (D == 0) protected_n += x[k] == 0xffffffffu;
+    if (D == 0 || ((x[k] ^ bar.value) >> digit_shift(D > 0 ? D - 1 : 0)) == 0)
+      atomicAdd(&hist[(x[k] >> digit_shift(D)) & digit_mask(D)], 1);
   }
   int all;
   block_scan(protected_n, wave_sums, &all);   // (and the counts are complete)
+  int32_t* const h = p.hist + (int64_t)b * HIST;
   if (D == 0 && tid == 0 && all > 0) atomicAdd(&h[3 * BINS], all);
   for (int i = tid; i < BINS; i += SEL_THREADS)
     if (hist[i] != 0) atomicAdd(&h[D * BINS + i], hist[i]);
 }
 
-__global__ __launch_bounds__(SEL_THREADS) void evict_count_kernel(const EvictParams p) {
-  __shared__ int wave_sums[SEL_WAVES];
-  __shared__ int found[2];
-  __shared__ int counts[4];
-  int begin = 0;
-  const int b = find_chunk(p, blockIdx.x, &begin), tid = threadIdx.x;
-  if (b < 0) return;
-  const EvictSeq sq(p, b);
-  if (tid < 4) counts[tid] = 0;
-  const Bar bar = bar_of<3>(p, sq, b, wave_sums, found);
-  __syncthreads();
-  const int i0 = ((int)blockIdx.x - begin) * CHUNK, i1 = min(sq.n, i0 + CHUNK);
-  int c[4] = {0, 0, 0, 0};
-  for (int i = i0 + tid; i < i1; i += SEL_THREADS) {
-    const uint32_t x = sq.key(i);
-    const bool up = bar.keep > 0 && x > bar.value, at = x == bar.value;
-    c[0] += up;
-    c[1] += at;
-    c[2] += up && i < bar.keep;
-    c[3] += at && i < bar.keep;
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) c[k] += __shfl_xor(c[k], o, 64);
-    if ((tid & 63) == 0) atomicAdd(&counts[k], c[k]);
-  }
-  __syncthreads();
-  if (tid < 4) p.chunk[(int64_t)blockIdx.x * 4 + tid] = counts[tid];
-}
-
-__global__ __launch_bounds__(SEL_THREADS) void evict_list_kernel(const EvictParams p) {
+// LIST false: the counts of every chunk. True: the moves, given those.
+template <bool LIST>
+__global__ __launch_bounds__(SEL_THREADS) void evict_chunk_kernel(const EvictParams p) {
   __shared__ int wave_sums[SEL_WAVES];
   __shared__ int found[2];
   __shared__ int counts[SEL_WAVES][4];
   int begin = 0;
-  const int b = find_chunk(p, blockIdx.x, &begin), tid = threadIdx.x;
+  EvictSeq sq;
+  const int b = find_chunk(p, blockIdx.x, &begin, &sq), tid = threadIdx.x;
   if (b < 0) return;
   const int lane = tid & 63, wave = tid >> 6;
-  const EvictSeq sq(p, b);
-  const Bar bar = bar_of<3>(p, sq, b, wave_sums, found);
-  const int keep = bar.keep, ties = bar.ties;
   const int i0 = ((int)blockIdx.x - begin) * CHUNK, i1 = min(sq.n, i0 + CHUNK);
-  constexpr int PART = CHUNK / SEL_WAVES, PER = PART / 64;
   const int p0 = min(i1, i0 + wave * PART), p1 = min(i1, p0 + PART);
+  Bar<3> bar(p, b);
   uint32_t x[PER];
-#pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const int i = p0 + k * 64 + lane;
-    x[k] = i < p1 ? sq.key(i) : 0;
-  }
+  load_keys(p, sq, p0 + lane, 64, p1, x);
+  int4 before = make_int4(0, 0, 0, 0);   // of the first 64 chunks before, a lane each
+  if (LIST && begin + lane < (int)blockIdx.x) before = *(const int4*)(p.chunk + (int64_t)(begin + lane) * 4);
+  bar.find(sq, wave_sums, found);
+  const int keep = bar.keep, ties = bar.ties;
   int c[4] = {0, 0, 0, 0};
 #pragma unroll
-  for (int k = 0; k < PER; ++k) {
-    const int i = p0 + k * 64 + lane;
-    const uint64_t up = __builtin_amdgcn_ballot_w64(i < p1 && keep > 0 && x[k] > bar.value);
-    const uint64_t at = __builtin_amdgcn_ballot_w64(i < p1 && x[k] == bar.value);
-    const int left = keep - (p0 + k * 64);
-    const uint64_t front = left <= 0 ? 0 : left >= 64 ? ~0ull : (1ull << left) - 1;
-    c[0] += __builtin_popcountll(up);
-    c[1] += __builtin_popcountll(at);
-    c[2] += __builtin_popcountll(up & front);
-    c[3] += __builtin_popcountll(at & front);
-  }
+  for (int k = 0; k < PER; ++k)
+    count_slots(p0 + k * 64, p0 + k * 64 + lane < p1, x[k], keep, bar.value, c);
   if (lane == 0)
 #pragma unroll
     for (int k = 0; k < 4; ++k) counts[wave][k] = c[k];
   __syncthreads();
+  if (!LIST) {
+    if (tid < 4) {
+      int sum = 0;
+#pragma unroll
+      for (int w = 0; w < SEL_WAVES; ++w) sum += counts[w][tid];
+      p.chunk[(int64_t)blockIdx.x * 4 + tid] = sum;
+    }
+    return;
+  }
   Ranks r = {0, 0, 0};
-  auto pass = [&](const int* n4, int first, int last) {   // the slots [first, last) and their counts
-    if (keep == sq.n) return;
+  // the slots [first, last) and their counts
+  auto pass = [&](const int* n4, int first, int last) {
     const int left = max(0, ties - r.ties);
     const int front = n4[2] + min(left, n4[3]);
     r.holes += min(keep, last) - min(keep, first) - front;
     r.movers += n4[0] + min(left, n4[1]) - front;
     r.ties += n4[1];
   };
-  if (keep < sq.n) {   // the chunks before, a lane each
+  if (keep < sq.n) {
     for (int k0 = begin; k0 < (int)blockIdx.x; k0 += 64) {
       const int k = k0 + lane;
       const bool in = k < (int)blockIdx.x;
-      const int4 y = in ? *(const int4*)(p.chunk + (int64_t)k * 4) : make_int4(0, 0, 0, 0);
+      const int4 y = k0 == begin ? before
+                     : in ? *(const int4*)(p.chunk + (int64_t)k * 4) : make_int4(0, 0, 0, 0);
       int end = y.y;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -471,26 +478,30 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_list_kernel(const EvictPara
       r.movers += movers;
       r.ties += __shfl(end, 63, 64);
     }
+    for (int w = 0; w < wave; ++w)
+      pass(counts[w], min(i1, i0 + w * PART), min(i1, i0 + (w + 1) * PART));
   }
-  for (int w = 0; w < wave; ++w)
-    pass(counts[w], min(i1, i0 + w * PART), min(i1, i0 + (w + 1) * PART));
-  if (keep < sq.n || !p.in_place) list_moves(p, sq, p0, p1, keep, bar.value, ties, r, [&](int i) { return sq.key(i); });
   if (i1 == sq.n && wave == SEL_WAVES - 1) {
-    pass(counts[wave], p0, p1);
+    const Ranks at = r;
+    if (keep < sq.n) pass(counts[wave], p0, p1);
     if (lane == 0) {
-      p.count[3 * b] = keep;
-      p.count[3 * b + 1] = r.holes;
-      p.count[3 * b + 2] = sq.n;
+      p.count[2 * b] = keep;
+      p.count[2 * b + 1] = r.holes;
     }
+    r = at;
+  }
+  if (keep < sq.n || !p.in_place) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+      list_moves(p, sq, p0 + k * 64, p0 + k * 64 + lane < p1, x[k], keep, bar.value, ties, r);
   }
 }
 
-// Rows and bookkeeping: in place the moves, otherwise all slots that are filled; and what is behind.
+// Rows and bookkeeping: in place the moves, otherwise all slots that are filled, and those behind.
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
   const int b = blockIdx.y;
   const Range from = range_of(p.cu, b, p.slots), to = range_of(p.cu_to, b, p.slots_to);
-  // (`used` is written below, and in place it is the one that was read: the count before is listed)
-  const int keep = p.count[3 * b], moves = p.count[3 * b + 1], n = p.count[3 * b + 2];
+  const int keep = p.count[2 * b], moves = p.count[2 * b + 1];
   const int64_t s0 = from.first, d0 = to.first;
   const int stride = gridDim.x * 256, first = blockIdx.x * 256 + threadIdx.x;
   const int rows = p.in_place ? moves : keep;
@@ -510,17 +521,19 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
     p.k_to[dst] = k;
     p.v_to[dst] = v;
     if (c == 0) {
-      // (in place the movers' own entries may be cleared already: theirs were listed)
-      const int t = p.in_place ? i : -1 - p.to[s0 + i];
-      p.pos_to[d0 + d] = t >= 0 ? p.from_pos[s0 + t] : p.kv_pos[s0 + s];
-      p.weight_to[d0 + d] = t >= 0 ? p.from_weight[s0 + t] : p.weight[s0 + s];
+      p.pos_to[d0 + d] = p.kv_pos[s0 + s];
+      p.weight_to[d0 + d] = p.weight[s0 + s];
+      if (p.in_place) {   // (no other thread reads the slot's entries)
+        p.kv_pos[s0 + s] = CP_POS_PAD_KV;
+        p.weight[s0 + s] = 0.f;
+      }
     }
   }
-  const int64_t end = p.in_place ? n : to.room;
-  for (int64_t i = keep + first; i < end; i += stride) {
-    p.pos_to[d0 + i] = CP_POS_PAD_KV;
-    p.weight_to[d0 + i] = 0.f;
-  }
+  if (!p.in_place)
+    for (int64_t i = keep + first; i < to.room; i += stride) {
+      p.pos_to[d0 + i] = CP_POS_PAD_KV;
+      p.weight_to[d0 + i] = 0.f;
+    }
   if (first == 0) p.used_to[b] = keep;
 }
 
@@ -541,10 +554,10 @@ EvictPlan evict_plan(const cp_shape& s) {
   pl.chunked = s.total_kv / s.batch > kChunkedSlots;
   pl.chunks = s.total_kv / CHUNK + s.batch;
   pl.list = round256((size_t)s.total_kv * 4);
-  pl.count = round256((size_t)s.batch * 12);
+  pl.count = round256((size_t)s.batch * 8);
   pl.hist = pl.chunked ? round256((size_t)s.batch * HIST * 4) : 0;
   pl.chunk = pl.chunked ? round256((size_t)pl.chunks * 16) : 0;
-  pl.bytes = 4 * pl.list + pl.count + pl.hist + pl.chunk;
+  pl.bytes = 2 * pl.list + pl.count + pl.hist + pl.chunk;
   return pl;
 }
 
@@ -609,8 +622,6 @@ extern "C" int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, 
   };
   p.to = (int32_t*)take(pl.list);
   p.from = (int32_t*)take(pl.list);
-  p.from_pos = (int32_t*)take(pl.list);
-  p.from_weight = (float*)take(pl.list);
   p.count = (int32_t*)take(pl.count);
   p.hist = (int32_t*)take(pl.hist);
   p.chunk = (int32_t*)take(pl.chunk);
@@ -622,8 +633,8 @@ extern "C" int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, 
     hipLaunchKernelGGL(evict_digit_kernel<0>, grid, block, 0, st, p);
     hipLaunchKernelGGL(evict_digit_kernel<1>, grid, block, 0, st, p);
     hipLaunchKernelGGL(evict_digit_kernel<2>, grid, block, 0, st, p);
-    hipLaunchKernelGGL(evict_count_kernel, grid, block, 0, st, p);
-    hipLaunchKernelGGL(evict_list_kernel, grid, block, 0, st, p);
+    hipLaunchKernelGGL(evict_chunk_kernel<false>, grid, block, 0, st, p);
+    hipLaunchKernelGGL(evict_chunk_kernel<true>, grid, block, 0, st, p);
   } else {
     // (a batch of more sequences than CUs: two workgroups share one)
     const int64_t most = s.batch > 256 ? kCachedKeys / 4 : kCachedKeys;
