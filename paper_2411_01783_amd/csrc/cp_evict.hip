@@ -73,27 +73,37 @@ __device__ __forceinline__ uint32_t key_of(float w, bool safe) {
   return (x & 0x80000000u) ? ~x : x | 0x80000000u;
 }
 
+// Inclusive prefix sums on the vector pipe (data-parallel moves between lanes; a __shfl is a round
+// trip through LDS): over 16 lanes, over the wavefront.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int x) {   // 0 where no lane moves here
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true);
+}
+__device__ __forceinline__ int row_scan(int x) {
+  x += moved<0x111, 0xf>(x);   // row_shr:1, 2, 4, 8
+  x += moved<0x112, 0xf>(x);
+  x += moved<0x114, 0xf>(x);
+  x += moved<0x118, 0xf>(x);
+  return x;
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  x = row_scan(x);
+  x += moved<0x142, 0xa>(x);   // lane 15 of a row to the next one: rows 1 and 3
+  x += moved<0x143, 0xc>(x);   // lane 31 to the upper half
+  return x;
+}
+
 // Prefix sum over the workgroup of x (exclusive), and the total.
 __device__ __forceinline__ int block_scan(int x, int* wave_sums, int* total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int end = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(end, o, 64);
-    if (lane >= o) end += y;
-  }
+  static_assert(SEL_WAVES == 16, "the wavefronts' sums are one row of lanes");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int end = wave_scan(x);
   __syncthreads();
   if (lane == 63) wave_sums[wave] = end;
   __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < SEL_WAVES; ++w) {
-    const int y = wave_sums[w];
-    if (w < wave) before += y;
-    all += y;
-  }
-  *total = all;
-  return before + end - x;
+  const int sums = row_scan(wave_sums[lane & 15]);
+  *total = __builtin_amdgcn_readlane(sums, 15);
+  return (wave > 0 ? __builtin_amdgcn_readlane(sums, wave - 1) : 0) + end - x;
 }
 
 // What a sequence keeps, and its slots' keys.
@@ -109,12 +119,15 @@ struct EvictSeq {
     budget = p.budget[b];
   }
   __device__ __forceinline__ EvictSeq of_lane(int l) const {
+    // (slots are counted in 31 bits; in scalar registers from here on)
     EvictSeq r;
-    r.src.first = __shfl(src.first, l, 64); r.src.room = __shfl(src.room, l, 64);
-    r.dst.first = __shfl(dst.first, l, 64); r.dst.room = __shfl(dst.room, l, 64);
-    r.n = __shfl(n, l, 64);
-    r.from_pos = __shfl(from_pos, l, 64);
-    r.budget = __shfl(budget, l, 64);
+    r.src.first = __builtin_amdgcn_readlane((int)src.first, l);
+    r.src.room = __builtin_amdgcn_readlane((int)src.room, l);
+    r.dst.first = __builtin_amdgcn_readlane((int)dst.first, l);
+    r.dst.room = __builtin_amdgcn_readlane((int)dst.room, l);
+    r.n = __builtin_amdgcn_readlane(n, l);
+    r.from_pos = __builtin_amdgcn_readlane(from_pos, l);
+    r.budget = __builtin_amdgcn_readlane(budget, l);
     return r;
   }
   __device__ __forceinline__ uint32_t key(const EvictParams& p, int32_t at, float w) const {
@@ -164,8 +177,8 @@ __device__ __forceinline__ int find_digit(int c1, int c0, int& left, int* wave_s
     found[1] = above + c1;
   }
   __syncthreads();
-  left -= found[1];
-  return found[0];
+  left -= __builtin_amdgcn_readfirstlane(found[1]);
+  return __builtin_amdgcn_readfirstlane(found[0]);
 }
 __device__ constexpr int digit_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
 __device__ constexpr uint32_t digit_mask(int d) { return d == 2 ? 1023u : 2047u; }
@@ -174,28 +187,40 @@ __device__ constexpr uint32_t digit_mask(int d) { return d == 2 ? 1023u : 2047u;
 struct Ranks {
   int ties, holes, movers;
 };
-// The 64 slots from g on (`in`: there is one for this lane, with key x): moves are listed, and in
-// place the bookkeeping of what goes is cleared. (Keys are read by the wavefront that lists them.)
-__device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq& sq, int g, bool in, uint32_t x,
+// The lanes in front of `end` of 64 slots from g on.
+__device__ __forceinline__ uint64_t lanes_before(int g, int end) {
+  const int left = end - g;
+  return left <= 0 ? 0 : left >= 64 ? ~0ull : (1ull << left) - 1;
+}
+__device__ __forceinline__ int rank_in(uint64_t mask) {   // set lanes in front of this one
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+// The slots [g, g + 64) in front of `end`, this lane's of key x: moves are listed, and in place the
+// bookkeeping of what goes is cleared. (Keys are read by the wavefront that lists them.) Which slots
+// stay is a matter of lane masks, in scalar registers; lanes are asked only where there is a move.
+__device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq& sq, int g, int end, uint32_t x,
                                            int keep, uint32_t bar, int ties, Ranks& r) {
-  const int lane = threadIdx.x & 63, i = g + lane;
-  const uint64_t below = (1ull << lane) - 1;
-  const bool tie = in && keep < sq.n && x == bar;
-  const uint64_t tied = __builtin_amdgcn_ballot_w64(tie);
-  const bool stays = in && keep > 0 && (keep == sq.n || x > bar ||
-                                        (tie && r.ties + __builtin_popcountll(tied & below) < ties));
-  r.ties += __builtin_popcountll(tied);
-  const bool hole = in && i < keep && !stays, mover = in && i >= keep && stays;
-  const uint64_t holes = __builtin_amdgcn_ballot_w64(hole), movers = __builtin_amdgcn_ballot_w64(mover);
-  if (hole) {
-    const int t = r.holes + __builtin_popcountll(holes & below);
-    if (p.in_place) p.to[sq.src.first + t] = i;
-    else p.to[sq.src.first + i] = -1 - t;
-  } else if (!p.in_place && in && i < keep) {
-    p.to[sq.src.first + i] = i;
+  const int i = g + (int)(threadIdx.x & 63);
+  const uint64_t in = lanes_before(g, end), front = lanes_before(g, keep) & in;
+  uint64_t stays = in;
+  if (keep < sq.n) {
+    const uint64_t up = __builtin_amdgcn_ballot_w64(x > bar) & in, at = __builtin_amdgcn_ballot_w64(x == bar) & in;
+    const int left = ties - r.ties, tied = __builtin_popcountll(at);
+    uint64_t kept = at;
+    if (left <= 0) kept = 0;
+    else if (left < tied) kept = __builtin_amdgcn_ballot_w64(rank_in(at) < left) & at;
+    stays = keep > 0 ? up | kept : 0;
+    r.ties += tied;
   }
-  if (mover) p.from[sq.src.first + r.movers + __builtin_popcountll(movers & below)] = i;
-  if (p.in_place && in && i >= keep && !stays) {
+  const uint64_t holes = front & ~stays, movers = stays & ~front, gone = in & ~front & ~stays;
+  auto mine = [&](uint64_t m) { return ((m >> (threadIdx.x & 63)) & 1) != 0; };
+  if (!p.in_place && front != 0) {
+    if (mine(front)) p.to[sq.src.first + i] = mine(holes) ? -1 - (r.holes + rank_in(holes)) : i;
+  } else if (holes != 0) {
+    if (mine(holes)) p.to[sq.src.first + r.holes + rank_in(holes)] = i;
+  }
+  if (movers != 0 && mine(movers)) p.from[sq.src.first + r.movers + rank_in(movers)] = i;
+  if (p.in_place && gone != 0 && mine(gone)) {
     p.kv_pos[sq.src.first + i] = CP_POS_PAD_KV;
     p.weight[sq.src.first + i] = 0.f;
   }
@@ -203,16 +228,39 @@ __device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq&
   r.movers += __builtin_popcountll(movers);
 }
 
-// Slots above the bar and at it among the 64 from g on, all of them and those in front of `keep`.
-__device__ __forceinline__ void count_slots(int g, bool in, uint32_t x, int keep, uint32_t bar, int (&c)[4]) {
-  const uint64_t up = __builtin_amdgcn_ballot_w64(in && keep > 0 && x > bar);
-  const uint64_t at = __builtin_amdgcn_ballot_w64(in && x == bar);
-  const int left = keep - g;
-  const uint64_t front = left <= 0 ? 0 : left >= 64 ? ~0ull : (1ull << left) - 1;
+// Slots above the bar and at it among [g, g + 64) in front of `end`, all and those in front of `keep`.
+__device__ __forceinline__ void count_slots(int g, int end, uint32_t x, int keep, uint32_t bar, int (&c)[4]) {
+  const uint64_t in = lanes_before(g, end), front = lanes_before(g, keep);
+  const uint64_t up = keep > 0 ? __builtin_amdgcn_ballot_w64(x > bar) & in : 0;
+  const uint64_t at = __builtin_amdgcn_ballot_w64(x == bar) & in;
   c[0] += __builtin_popcountll(up);
   c[1] += __builtin_popcountll(at);
   c[2] += __builtin_popcountll(up & front);
   c[3] += __builtin_popcountll(at & front);
+}
+
+// Parts of a sequence, one a lane in their order, by their counts y: added to `r` what the parts before
+// part `a` hold, and to `e` what those before part `z` do. The first part begins behind the r.ties
+// (e.ties) ties that there are so far.
+__device__ __forceinline__ void add_parts(bool in, int4 y, int first, int last, int keep, int ties, int a,
+                                          Ranks& r, int z, Ranks& e) {
+  const int tied = wave_scan(y.y);
+  const int left = max(0, ties - (r.ties + tied - y.y));
+  const int front = y.z + min(left, y.w);
+  const int holes = wave_scan(in ? min(keep, last) - min(keep, first) - front : 0);
+  const int movers = wave_scan(in ? y.x + min(left, y.y) - front : 0);
+  auto add = [&](int k, Ranks& to) {   // k uniform
+    if (k == 0) return;
+    to.ties += __builtin_amdgcn_readlane(tied, k - 1);
+    to.holes += __builtin_amdgcn_readlane(holes, k - 1);
+    to.movers += __builtin_amdgcn_readlane(movers, k - 1);
+  };
+  const Ranks base = r;
+  add(a, r);
+  if (&e != &r) {
+    e = base;
+    add(z, e);
+  }
 }
 
 // A workgroup per sequence. The keys of the first `cached` slots are kept in LDS.
@@ -221,7 +269,8 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
   __shared__ int hist[BINS];
   __shared__ int wave_sums[SEL_WAVES];
   __shared__ int found[2];
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const EvictSeq sq(p, b);
   for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
   __syncthreads();
@@ -271,35 +320,24 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
     const int i0 = min(sq.n, wave * part), i1 = min(sq.n, i0 + part);
     int c[4] = {0, 0, 0, 0};
     for (int g = i0; g < i1; g += 64) {
-      const bool in = g + lane < i1;
-      count_slots(g, in, in ? key(g + lane) : 0, keep, bar, c);
+      count_slots(g, i1, g + lane < i1 ? key(g + lane) : 0, keep, bar, c);
     }
-    __shared__ int counts[SEL_WAVES][4];
+    __shared__ __align__(16) int counts[SEL_WAVES][4];
     if (lane == 0)
 #pragma unroll
       for (int k = 0; k < 4; ++k) counts[wave][k] = c[k];
     __syncthreads();
     // ... then their ranks
-    Ranks r = {0, 0, 0};
-    for (int w = 0; w < wave; ++w) {
-      const int w0 = min(sq.n, w * part), size = min(keep, min(sq.n, w0 + part)) - min(keep, w0);
-      const int left = max(0, ties - r.ties);
-      const int front = counts[w][2] + min(left, counts[w][3]);
-      r.holes += size - front;
-      r.movers += counts[w][0] + min(left, counts[w][1]) - front;
-      r.ties += counts[w][1];
+    Ranks r = {0, 0, 0}, end = {0, 0, 0};
+    {
+      const int w0 = min(sq.n, lane * part), w1 = min(sq.n, w0 + part);
+      add_parts(lane < SEL_WAVES, lane < SEL_WAVES ? *(const int4*)counts[lane] : make_int4(0, 0, 0, 0), w0, w1,
+                keep, ties, wave, r, SEL_WAVES, end);
     }
-    const Ranks before = r;
     for (int g = i0; g < i1; g += 64) {
-      const bool in = g + lane < i1;
-      list_moves(p, sq, g, in, in ? key(g + lane) : 0, keep, bar, ties, r);
+      list_moves(p, sq, g, i1, g + lane < i1 ? key(g + lane) : 0, keep, bar, ties, r);
     }
-    r = before;
-    if (wave == SEL_WAVES - 1 && lane == 0) {
-      const int left = max(0, ties - r.ties);
-      const int size = min(keep, i1) - min(keep, i0);
-      p.count[2 * b + 1] = r.holes + size - (c[2] + min(left, c[3]));
-    }
+    if (tid == 0) p.count[2 * b + 1] = end.holes;
   } else {
     if (!p.in_place)
       for (int i = tid; i < keep; i += SEL_THREADS) p.to[sq.src.first + i] = i;
@@ -319,20 +357,15 @@ __device__ __forceinline__ int find_chunk(const EvictParams& p, int x, int* begi
     const bool in = b0 + lane < p.batch;
     const EvictSeq mine(p, in ? b0 + lane : b0);
     const int c = in ? (mine.n + CHUNK - 1) / CHUNK : 0;
-    int end = c;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(end, o, 64);
-      if (lane >= o) end += y;
-    }
+    const int end = wave_scan(c);
     const uint64_t behind = __builtin_amdgcn_ballot_w64(base + end > x);
     if (behind != 0) {
       const int l = __builtin_ctzll(behind);
-      *begin = base + __shfl(end - c, l, 64);
+      *begin = base + __builtin_amdgcn_readlane(end - c, l);
       *sq = mine.of_lane(l);
       return b0 + l;
     }
-    base += __shfl(end, 63, 64);
+    base += __builtin_amdgcn_readlane(end, 63);
   }
   return -1;
 }
@@ -362,7 +395,7 @@ struct Bar {
   }
   // (uniform)
   __device__ __forceinline__ void find(const EvictSeq& sq, int* wave_sums, int* found) {
-    keep = ties = sq.keep(protected_n);
+    keep = ties = sq.keep(__builtin_amdgcn_readfirstlane(protected_n));
     if (keep == 0 || keep == sq.n) return;
 #pragma unroll
     for (int d = 0; d < STEP; ++d)
@@ -412,12 +445,12 @@ template <bool LIST>
 __global__ __launch_bounds__(SEL_THREADS) void evict_chunk_kernel(const EvictParams p) {
   __shared__ int wave_sums[SEL_WAVES];
   __shared__ int found[2];
-  __shared__ int counts[SEL_WAVES][4];
+  __shared__ __align__(16) int counts[SEL_WAVES][4];
   int begin = 0;
   EvictSeq sq;
   const int b = find_chunk(p, blockIdx.x, &begin, &sq), tid = threadIdx.x;
   if (b < 0) return;
-  const int lane = tid & 63, wave = tid >> 6;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i0 = ((int)blockIdx.x - begin) * CHUNK, i1 = min(sq.n, i0 + CHUNK);
   const int p0 = min(i1, i0 + wave * PART), p1 = min(i1, p0 + PART);
   Bar<3> bar(p, b);
@@ -430,7 +463,7 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_chunk_kernel(const EvictPar
   int c[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int k = 0; k < PER; ++k)
-    count_slots(p0 + k * 64, p0 + k * 64 + lane < p1, x[k], keep, bar.value, c);
+    count_slots(p0 + k * 64, p1, x[k], keep, bar.value, c);
   if (lane == 0)
 #pragma unroll
     for (int k = 0; k < 4; ++k) counts[wave][k] = c[k];
@@ -444,56 +477,28 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_chunk_kernel(const EvictPar
     }
     return;
   }
-  Ranks r = {0, 0, 0};
-  // the slots [first, last) and their counts
-  auto pass = [&](const int* n4, int first, int last) {
-    const int left = max(0, ties - r.ties);
-    const int front = n4[2] + min(left, n4[3]);
-    r.holes += min(keep, last) - min(keep, first) - front;
-    r.movers += n4[0] + min(left, n4[1]) - front;
-    r.ties += n4[1];
-  };
+  Ranks r = {0, 0, 0}, end = {0, 0, 0};
   if (keep < sq.n) {
-    for (int k0 = begin; k0 < (int)blockIdx.x; k0 += 64) {
+    const int mine = (int)blockIdx.x - begin;   // chunks before
+    for (int k0 = 0; k0 < mine; k0 += 64) {
       const int k = k0 + lane;
-      const bool in = k < (int)blockIdx.x;
-      const int4 y = k0 == begin ? before
-                     : in ? *(const int4*)(p.chunk + (int64_t)k * 4) : make_int4(0, 0, 0, 0);
-      int end = y.y;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const int z = __shfl_up(end, o, 64);
-        if (lane >= o) end += z;
-      }
-      const int left = max(0, ties - (r.ties + end - y.y));
-      const int front = y.z + min(left, y.w);
-      const int size = min(keep, (k - begin + 1) * CHUNK) - min(keep, (k - begin) * CHUNK);
-      int holes = in ? size - front : 0, movers = in ? y.x + min(left, y.y) - front : 0;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) {
-        holes += __shfl_xor(holes, o, 64);
-        movers += __shfl_xor(movers, o, 64);
-      }
-      r.holes += holes;
-      r.movers += movers;
-      r.ties += __shfl(end, 63, 64);
+      const bool in = k < mine;
+      const int4 y = k0 == 0 ? before
+                     : in ? *(const int4*)(p.chunk + (int64_t)(begin + k) * 4) : make_int4(0, 0, 0, 0);
+      add_parts(in, y, k * CHUNK, (k + 1) * CHUNK, keep, ties, min(64, mine - k0), r, 0, r);
     }
-    for (int w = 0; w < wave; ++w)
-      pass(counts[w], min(i1, i0 + w * PART), min(i1, i0 + (w + 1) * PART));
+    const int w0 = min(i1, i0 + lane * PART), w1 = min(i1, w0 + PART);
+    add_parts(lane < SEL_WAVES, lane < SEL_WAVES ? *(const int4*)counts[lane] : make_int4(0, 0, 0, 0), w0, w1,
+              keep, ties, wave, r, SEL_WAVES, end);
   }
-  if (i1 == sq.n && wave == SEL_WAVES - 1) {
-    const Ranks at = r;
-    if (keep < sq.n) pass(counts[wave], p0, p1);
-    if (lane == 0) {
-      p.count[2 * b] = keep;
-      p.count[2 * b + 1] = r.holes;
-    }
-    r = at;
+  if (i1 == sq.n && tid == 0) {
+    p.count[2 * b] = keep;
+    p.count[2 * b + 1] = end.holes;
   }
   if (keep < sq.n || !p.in_place) {
 #pragma unroll
     for (int k = 0; k < PER; ++k)
-      list_moves(p, sq, p0 + k * 64, p0 + k * 64 + lane < p1, x[k], keep, bar.value, ties, r);
+      list_moves(p, sq, p0 + k * 64, p1, x[k], keep, bar.value, ties, r);
   }
 }
 
