@@ -198,9 +198,9 @@ __device__ __forceinline__ int rank_in(uint64_t mask) {   // set lanes in front 
 // The slots [g, g + 64) in front of `end`, this lane's of key x: moves are listed, and in place the
 // bookkeeping of what goes is cleared. (Keys are read by the wavefront that lists them.) Which slots
 // stay is a matter of lane masks, in scalar registers; lanes are asked only where there is a move.
-__device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq& sq, int g, int end, uint32_t x,
+__device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq& sq, int g0, int end, uint32_t x,
                                            int keep, uint32_t bar, int ties, Ranks& r) {
-  const int i = g + (int)(threadIdx.x & 63);
+  const int g = __builtin_amdgcn_readfirstlane(g0), i = g + (int)(threadIdx.x & 63);
   const uint64_t in = lanes_before(g, end), front = lanes_before(g, keep) & in;
   uint64_t stays = in;
   if (keep < sq.n) {
@@ -229,7 +229,8 @@ __device__ __forceinline__ void list_moves(const EvictParams& p, const EvictSeq&
 }
 
 // Slots above the bar and at it among [g, g + 64) in front of `end`, all and those in front of `keep`.
-__device__ __forceinline__ void count_slots(int g, int end, uint32_t x, int keep, uint32_t bar, int (&c)[4]) {
+__device__ __forceinline__ void count_slots(int g0, int end, uint32_t x, int keep, uint32_t bar, int (&c)[4]) {
+  const int g = __builtin_amdgcn_readfirstlane(g0);
   const uint64_t in = lanes_before(g, end), front = lanes_before(g, keep);
   const uint64_t up = keep > 0 ? __builtin_amdgcn_ballot_w64(x > bar) & in : 0;
   const uint64_t at = __builtin_amdgcn_ballot_w64(x == bar) & in;
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
   for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
   __syncthreads();
   int protected_n = 0;
-  constexpr int AT_ONCE = 8;
+  constexpr int AT_ONCE = 8;   // keys of a lane in flight
   for (int i0 = tid; i0 < sq.n; i0 += AT_ONCE * SEL_THREADS) {
     uint32_t x[AT_ONCE];
     load_keys(p, sq, i0, SEL_THREADS, sq.n, x);
@@ -291,7 +292,21 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
   int all;
   block_scan(protected_n, wave_sums, &all);   // (and the counts are complete)
   const int keep = sq.keep(all);
-  auto key = [&](int i) -> uint32_t { return i < cached ? keys[i] : sq.key(p, i); };
+  // f(i, key of slot i) for the slots i, i + step, ... in front of `end` (behind it with a key of 0, up
+  // to AT_ONCE steps), the keys of AT_ONCE slots requested together
+  auto each_key = [&](int i0, int step, int end, auto f) {
+    for (int i = i0; __builtin_amdgcn_ballot_w64(i < end) != 0; i += AT_ONCE * step) {
+      uint32_t x[AT_ONCE];
+      if (sq.n <= cached) {
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) x[k] = keys[min(i + k * step, sq.n - 1)];
+      } else {
+        load_keys(p, sq, i, step, end, x);
+      }
+#pragma unroll
+      for (int k = 0; k < AT_ONCE; ++k) f(i + k * step, x[k]);
+    }
+  };
 
   // the key of the last slot that stays, and how many slots with that key do
   uint32_t bar = 0;
@@ -304,10 +319,10 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
         for (int i = tid; i < BINS; i += SEL_THREADS) hist[i] = 0;
         __syncthreads();
         const int above = digit_shift(d - 1);
-        for (int i = tid; i < sq.n; i += SEL_THREADS) {
-          const uint32_t x = key(i);
-          if (((x ^ bar) >> above) == 0) atomicAdd(&hist[(x >> digit_shift(d)) & digit_mask(d)], 1);
-        }
+        each_key(tid, SEL_THREADS, sq.n, [&](int i, uint32_t x) {
+          if (i < sq.n && ((x ^ bar) >> above) == 0)
+            atomicAdd(&hist[(x >> digit_shift(d)) & digit_mask(d)], 1);
+        });
         __syncthreads();
       }
       const int hi = BINS - 1 - 2 * tid;
@@ -319,9 +334,7 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
     const int part = ((sq.n + SEL_THREADS - 1) / SEL_THREADS) * 64;
     const int i0 = min(sq.n, wave * part), i1 = min(sq.n, i0 + part);
     int c[4] = {0, 0, 0, 0};
-    for (int g = i0; g < i1; g += 64) {
-      count_slots(g, i1, g + lane < i1 ? key(g + lane) : 0, keep, bar, c);
-    }
+    each_key(i0 + lane, 64, i1, [&](int i, uint32_t x) { count_slots(i - lane, i1, x, keep, bar, c); });
     __shared__ __align__(16) int counts[SEL_WAVES][4];
     if (lane == 0)
 #pragma unroll
@@ -334,9 +347,9 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
       add_parts(lane < SEL_WAVES, lane < SEL_WAVES ? *(const int4*)counts[lane] : make_int4(0, 0, 0, 0), w0, w1,
                 keep, ties, wave, r, SEL_WAVES, end);
     }
-    for (int g = i0; g < i1; g += 64) {
-      list_moves(p, sq, g, i1, g + lane < i1 ? key(g + lane) : 0, keep, bar, ties, r);
-    }
+    each_key(i0 + lane, 64, i1, [&](int i, uint32_t x) {
+      list_moves(p, sq, i - lane, i1, x, keep, bar, ties, r);
+    });
     if (tid == 0) p.count[2 * b + 1] = end.holes;
   } else {
     if (!p.in_place)
