@@ -12,7 +12,7 @@
 // over 64-slot ballots. Sequences that one workgroup reads quickly are one launch, a workgroup
 // each, with the keys in LDS; longer ones are cut into chunks and take a launch per digit. The last
 // launch moves the rows and does the bookkeeping.
-#include "cp_common.h"
+#include "cp_scan.h"
 
 namespace cp {
 namespace {
@@ -47,9 +47,6 @@ struct EvictParams {
   int32_t* chunk;   // [chunk][4]: slots above the bar, at it; the same in front of `keep`
 };
 
-__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
-  return x < lo ? lo : x > hi ? hi : x;
-}
 struct Range {
   int64_t first, room;
 };
@@ -71,26 +68,6 @@ __device__ __forceinline__ uint32_t key_of(float w, bool safe) {
   if (w != w) return 0;
   const uint32_t x = __builtin_bit_cast(uint32_t, w + 0.f);   // (-0 counts as 0)
   return (x & 0x80000000u) ? ~x : x | 0x80000000u;
-}
-
-// Inclusive prefix sums on the vector pipe (data-parallel moves between lanes; a __shfl is a round
-// trip through LDS): over 16 lanes, over the wavefront.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int moved(int x) {   // 0 where no lane moves here
-  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true);
-}
-__device__ __forceinline__ int row_scan(int x) {
-  x += moved<0x111, 0xf>(x);   // row_shr:1, 2, 4, 8
-  x += moved<0x112, 0xf>(x);
-  x += moved<0x114, 0xf>(x);
-  x += moved<0x118, 0xf>(x);
-  return x;
-}
-__device__ __forceinline__ int wave_scan(int x) {
-  x = row_scan(x);
-  x += moved<0x142, 0xa>(x);   // lane 15 of a row to the next one: rows 1 and 3
-  x += moved<0x143, 0xc>(x);   // lane 31 to the upper half
-  return x;
 }
 
 // Prefix sum over the workgroup of x (exclusive), and the total.
@@ -361,26 +338,11 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
 
 // ---- sequences in chunks, a workgroup each ----
 
-// The sequence that chunk x of all sequences belongs to (its number, what it holds), and its first
-// chunk. Everything that a lane's sequence is described by is requested at once.
+// The sequence that chunk x of all sequences belongs to, what it holds, and its first chunk.
 __device__ __forceinline__ int find_chunk(const EvictParams& p, int x, int* begin, EvictSeq* sq) {
-  const int lane = threadIdx.x & 63;
-  int base = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    const bool in = b0 + lane < p.batch;
-    const EvictSeq mine(p, in ? b0 + lane : b0);
-    const int c = in ? (mine.n + CHUNK - 1) / CHUNK : 0;
-    const int end = wave_scan(c);
-    const uint64_t behind = __builtin_amdgcn_ballot_w64(base + end > x);
-    if (behind != 0) {
-      const int l = __builtin_ctzll(behind);
-      *begin = base + __builtin_amdgcn_readlane(end - c, l);
-      *sq = mine.of_lane(l);
-      return b0 + l;
-    }
-    base += __builtin_amdgcn_readlane(end, 63);
-  }
-  return -1;
+  return find_sequence_of_block(
+      p.batch, x, begin, sq, [&](int b) { return EvictSeq(p, b); },
+      [](const EvictSeq& s) { return (s.n + CHUNK - 1) / CHUNK; });
 }
 
 __global__ __launch_bounds__(256) void evict_clear_kernel(const EvictParams p) {

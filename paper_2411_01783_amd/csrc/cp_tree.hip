@@ -17,7 +17,7 @@
 // shares leaves fp32 parts that a second launch joins (the merge of Appendix B, Equation 4).
 #include <math.h>
 
-#include "cp_common.h"
+#include "cp_scan.h"
 
 namespace cp {
 namespace {
@@ -63,9 +63,6 @@ struct TreeSeq {
   int32_t n, used;     // nodes, tokens in the cache
   int64_t spans, tiles;
 };
-__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
-  return x < lo ? lo : x > hi ? hi : x;
-}
 // RM rows of a row block, SPT sub-tiles of a tile
 template <int RM, int SPT>
 __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {

@@ -12,7 +12,7 @@
 // second launch adds them up in order.
 #include <math.h>
 
-#include "cp_common.h"
+#include "cp_scan.h"
 
 namespace cp {
 namespace {
@@ -38,46 +38,33 @@ struct WeightParams {
   float scale_log2, decay;
 };
 
-__device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
-  return x < lo ? lo : x > hi ? hi : x;
-}
 struct Seq {
-  int64_t q0, k0;
-  int32_t n, used;
+  int32_t q0, n, k0, used;   // first query, queries, first slot, tokens in the cache
+  __device__ __forceinline__ Seq of_lane(int l) const {
+    Seq r;
+    r.q0 = __builtin_amdgcn_readlane(q0, l);
+    r.n = __builtin_amdgcn_readlane(n, l);
+    r.k0 = __builtin_amdgcn_readlane(k0, l);
+    r.used = __builtin_amdgcn_readlane(used, l);
+    return r;
+  }
 };
 // (boundaries that contradict each other or the totals are cut to what is there)
 __device__ __forceinline__ Seq seq_of(const WeightParams& p, int b) {
+  const int32_t a0 = p.cu_q[b], a1 = p.cu_q[b + 1], c0 = p.cu_kv[b], c1 = p.cu_kv[b + 1];
+  const int32_t u = p.used != nullptr ? p.used[b] : INT32_MAX;
   Seq s;
-  s.q0 = clamp64(p.cu_q[b], 0, p.total_q);
-  s.n = (int32_t)(clamp64(p.cu_q[b + 1], s.q0, p.total_q) - s.q0);
-  s.k0 = clamp64(p.cu_kv[b], 0, p.total_kv);
-  const int64_t room = clamp64(p.cu_kv[b + 1], s.k0, p.total_kv) - s.k0;
-  s.used = (int32_t)(p.used != nullptr ? clamp64(p.used[b], 0, room) : room);
+  s.q0 = (int32_t)clamp64(a0, 0, p.total_q);
+  s.n = (int32_t)clamp64(a1, s.q0, p.total_q) - s.q0;
+  s.k0 = (int32_t)clamp64(c0, 0, p.total_kv);
+  s.used = (int32_t)clamp64(u, 0, clamp64(c1, s.k0, p.total_kv) - s.k0);
   return s;
 }
-
-// The sequence that block x of the line of all sequences' key blocks belongs to, and its first block.
-__device__ __forceinline__ int find_block(const WeightParams& p, int x, int* begin) {
-  const int lane = threadIdx.x & 63;
-  int base = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    int c = 0;
-    if (b0 + lane < p.batch) c = (seq_of(p, b0 + lane).used + p.wg_keys - 1) / p.wg_keys;
-    int end = c;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int y = __shfl_up(end, o, 64);
-      if (lane >= o) end += y;
-    }
-    const uint64_t behind = __builtin_amdgcn_ballot_w64(base + end > x);
-    if (behind != 0) {
-      const int l = __builtin_ctzll(behind);
-      *begin = base + __shfl(end - c, l, 64);
-      return b0 + l;
-    }
-    base += __shfl(end, 63, 64);
-  }
-  return -1;
+// The sequence that block x of all sequences' key blocks belongs to, and its first block.
+__device__ __forceinline__ int find_block(const WeightParams& p, int x, int* begin, Seq* sq) {
+  return find_sequence_of_block(
+      p.batch, x, begin, sq, [&](int b) { return seq_of(p, b); },
+      [&](const Seq& s) { return (s.used + p.wg_keys - 1) / p.wg_keys; });
 }
 
 __device__ __forceinline__ floatx16_t product(const uint4& a, const uint4& b, floatx16_t c, bf16_t) {
@@ -95,9 +82,9 @@ __device__ __forceinline__ floatx16_t product(const uint4& a, const uint4& b, fl
 // on by a constant number of rows.
 struct RowAt {
   int32_t node, head;
-  __device__ __forceinline__ void set(int64_t r, int group) {
+  __device__ __forceinline__ void set(uint32_t r, uint32_t group) {
     node = (int32_t)(r / group);
-    head = (int32_t)(r - (int64_t)node * group);
+    head = (int32_t)(r - (uint32_t)node * group);
   }
   __device__ __forceinline__ void advance(int by_node, int by_head, int group) {
     node += by_node;
@@ -109,11 +96,16 @@ struct RowAt {
   }
 };
 
-// KB: fragments of 32 keys that a wavefront holds. A tile of 64 rows travels through registers into
-// one of two LDS buffers while the tile before it is used (16-byte chunk c of row r lies at
-// c ^ (r % chunks): 16 lanes that read the same chunk of neighbouring rows touch all banks).
-template <typename TI, int D, int KB>
-__global__ __launch_bounds__(NW * 64, KB == 1 && sizeof(TI) == 2 ? 4 : 2) void kv_weight_kernel(const WeightParams p) {
+// KB: fragments of 32 keys that a wavefront holds. FLAT: one KV head, whose rows lie one behind the
+// other in Q. A tile of 64 rows travels through registers into one of two LDS buffers while the
+// tile before it is used (16-byte chunk c of row r lies at c ^ (r % chunks): 16 lanes that read the same
+// chunk of neighbouring rows touch all banks).
+// Bound by the exponentials: a score costs a wavefront 24 clocks of vector issue (fma, exp at a quarter
+// of the rate, add) and 16 of the matrix pipe, so the products of a row and key block are issued
+// between the exponentials of the one before it.
+template <typename TI, int D, int KB, bool FLAT>
+__global__ __launch_bounds__(NW * 64, KB == 1 && sizeof(TI) == 2 ? 4 : 2) void kv_weight_kernel(
+    const WeightParams p) {
   constexpr int ROW = D * (int)sizeof(TI), CH = ROW / 16, NKS = CH / 2;
   constexpr int ST = TILE * CH / (NW * 64);        // chunks of a tile that a lane brings
   constexpr int RPI = NW * 64 / CH;                // rows that the workgroup brings at a time
@@ -125,9 +117,8 @@ __global__ __launch_bounds__(NW * 64, KB == 1 && sizeof(TI) == 2 ? 4 : 2) void k
   __shared__ __align__(16) int32_t pos_of[2][NW][TILE];
   __shared__ int32_t wg_k_min[NW], wg_first[NW], wg_last[NW];
   int begin = 0;
-  const int b = find_block(p, blockIdx.x, &begin);
-  if (b < 0) return;
-  const Seq sq = seq_of(p, b);
+  Seq sq;
+  if (find_block(p, blockIdx.x, &begin, &sq) < 0) return;
   const int range = blockIdx.y % p.n_ranges, kvh = blockIdx.y / p.n_ranges;
   const int key0 = ((int)blockIdx.x - begin) * p.wg_keys + wave * KB * KEYS;
   const int64_t tok_q = (int64_t)p.n_q_heads * D, tok_kv = (int64_t)p.n_kv_heads * D;
@@ -135,15 +126,79 @@ __global__ __launch_bounds__(NW * 64, KB == 1 && sizeof(TI) == 2 ? 4 : 2) void k
   // lane (rl, hf): 16-byte chunk 2 ks + hf of key rl of the fragment (keys behind the last repeat it)
   uint4 kf[KB][NKS];
   int32_t kp[KB];
-  int32_t k_max = INT32_MIN, k_min = INT32_MAX;
 #pragma unroll
   for (int f = 0; f < KB; ++f) {
-    const int64_t key = sq.k0 + min(key0 + f * KEYS + rl, sq.used - 1);
+    const int64_t key = (int64_t)sq.k0 + min(key0 + f * KEYS + rl, sq.used - 1);
     kp[f] = p.kv_pos[key];
     const uint4* src = (const uint4*)((const TI*)p.k + key * tok_kv + kvh * D) + hf;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) kf[f][ks] = src[2 * ks];
   }
+  const int n_rows = sq.n * p.group;
+  const int tiles = (n_rows + TILE - 1) / TILE;
+  int t0 = (int)((int64_t)tiles * range / p.n_ranges), t1 = (int)((int64_t)tiles * (range + 1) / p.n_ranges);
+
+  // ---- a tile on its way: ST chunks of Q a lane, and of every row its LSE and position ----
+  const TI* const q0 = (const TI*)p.q + sq.q0 * tok_q;
+  const float* const lse0 = p.lse + (int64_t)sq.q0 * p.n_q_heads;
+  const int32_t* const pos0 = p.q_pos + sq.q0;
+  RowAt at[FLAT ? 1 : ST], mine;
+  const int by_node = TILE / p.group, by_head = TILE % p.group;
+  auto start = [&](int t) {
+    mine.set(t * TILE + lane, p.group);
+    if (!FLAT)
+#pragma unroll
+      for (int i = 0; i < ST; ++i) at[FLAT ? 0 : i].set(t * TILE + i * RPI + tid / CH, p.group);
+  };
+  uint4 st[ST];
+  float st_lse;
+  int32_t st_pos;
+  auto fetch = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < ST; ++i) {
+      st[i] = make_uint4(0, 0, 0, 0);
+      if (FLAT) {
+        const int r = t * TILE + i * RPI + tid / CH;
+        if (r < n_rows) st[i] = ((const uint4*)(q0 + (int64_t)r * D))[tid % CH];
+      } else {
+        RowAt& a = at[FLAT ? 0 : i];
+        if (a.node < sq.n)
+          st[i] = ((const uint4*)(q0 + a.node * tok_q + (kvh * p.group + a.head) * D))[tid % CH];
+        a.advance(by_node, by_head, p.group);
+      }
+    }
+    st_lse = INFINITY;
+    st_pos = INT32_MIN;
+    if (mine.node < sq.n) {
+      st_lse = FLAT ? lse0[t * TILE + lane] : lse0[(int64_t)mine.node * p.n_q_heads + kvh * p.group + mine.head];
+      st_pos = pos0[mine.node];
+    }
+    mine.advance(by_node, by_head, p.group);
+  };
+  // a row that sees no key anywhere (LSE = -inf), and one behind the last, weighs nothing
+  auto put = [&](int to) {
+#pragma unroll
+    for (int i = 0; i < ST; ++i) {
+      const int r = i * RPI + tid / CH;
+      *(uint4*)(tile[to] + r * ROW + (((tid % CH) ^ (r & (CH - 1))) << 4)) = st[i];
+    }
+    lse_of[to][wave][lane] = st_lse == -INFINITY ? INFINITY : st_lse * kLog2e;
+    pos_of[to][wave][lane] = st_pos;
+  };
+
+  const bool look = t1 - t0 > 2;
+  if (!look && t0 < t1) {   // (requested with the keys)
+    start(t0);
+    fetch(t0);
+  }
+  float old[KB];
+#pragma unroll
+  for (int f = 0; f < KB; ++f) {
+    old[f] = 0.f;
+    if (p.part == nullptr && p.decay != 0.f && key0 + f * KEYS + rl < sq.used)
+      old[f] = p.weight[(int64_t)sq.k0 + key0 + f * KEYS + rl];
+  }
+  int32_t k_max = INT32_MIN, k_min = INT32_MAX;
 #pragma unroll
   for (int f = 0; f < KB; ++f) {
     k_max = max(k_max, kp[f]);
@@ -154,24 +209,17 @@ __global__ __launch_bounds__(NW * 64, KB == 1 && sizeof(TI) == 2 ? 4 : 2) void k
     k_max = max(k_max, __shfl_xor(k_max, o, 64));
     k_min = min(k_min, __shfl_xor(k_min, o, 64));
   }
-
-  float sum[KB];
-#pragma unroll
-  for (int f = 0; f < KB; ++f) sum[f] = 0.f;
-  const int64_t n_rows = (int64_t)sq.n * p.group;
-  const int64_t tiles = (n_rows + TILE - 1) / TILE;
-  int64_t t0 = tiles * range / p.n_ranges, t1 = tiles * (range + 1) / p.n_ranges;
-  if (t1 - t0 > 2) {
+  if (look) {
     // the tiles between the first and the last row that sees any key of the workgroup
     if (lane == 0) wg_k_min[wave] = k_min;
     __syncthreads();
     int32_t lo = wg_k_min[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) lo = min(lo, wg_k_min[w]);
-    const int n0 = (int)(t0 * TILE / p.group), n1 = (int)min<int64_t>(sq.n, (t1 * TILE - 1) / p.group + 1);
+    const int n0 = t0 * TILE / p.group, n1 = min(sq.n, (t1 * TILE - 1) / p.group + 1);
     int first = INT32_MAX, last = -1;
     for (int i = n0 + tid; i < n1; i += NW * 64)
-      if (p.q_pos[sq.q0 + i] >= lo) {
+      if (pos0[i] >= lo) {
         first = min(first, i);
         last = i;
       }
@@ -190,105 +238,113 @@ __global__ __launch_bounds__(NW * 64, KB == 1 && sizeof(TI) == 2 ? 4 : 2) void k
       first = min(first, wg_first[w]);
       last = max(last, wg_last[w]);
     }
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
     if (last < 0) {
       t1 = t0;
     } else {
-      t0 = max(t0, (int64_t)first * p.group / TILE);
-      t1 = min(t1, ((int64_t)(last + 1) * p.group - 1) / TILE + 1);
+      t0 = max(t0, first * p.group / TILE);
+      t1 = min(t1, ((last + 1) * p.group - 1) / TILE + 1);
+    }
+    if (t0 < t1) {
+      start(t0);
+      fetch(t0);
     }
   }
+  if (t0 < t1) put(t0 & 1);
 
-  // ---- a tile on its way: ST chunks of Q a lane, and of every row its LSE and position ----
-  RowAt at[ST], mine;
+  float sum[KB];
 #pragma unroll
-  for (int i = 0; i < ST; ++i) at[i].set(t0 * TILE + i * RPI + tid / CH, p.group);
-  mine.set(t0 * TILE + lane, p.group);
-  const int by_node = TILE / p.group, by_head = TILE % p.group;
-  uint4 st[ST];
-  float st_lse;
-  int32_t st_pos;
-  auto fetch = [&]() {
-#pragma unroll
-    for (int i = 0; i < ST; ++i) {
-      st[i] = make_uint4(0, 0, 0, 0);
-      if (at[i].node < sq.n)
-        st[i] = ((const uint4*)((const TI*)p.q + (sq.q0 + at[i].node) * tok_q +
-                                (kvh * p.group + at[i].head) * D))[tid % CH];
-      at[i].advance(by_node, by_head, p.group);
-    }
-    st_lse = INFINITY;
-    st_pos = INT32_MIN;
-    if (mine.node < sq.n) {
-      st_lse = p.lse[(sq.q0 + mine.node) * p.n_q_heads + kvh * p.group + mine.head];
-      st_pos = p.q_pos[sq.q0 + mine.node];
-    }
-    mine.advance(by_node, by_head, p.group);
-  };
-  // a row that sees no key anywhere (LSE = -inf), and one behind the last, weighs nothing
-  auto put = [&](int to) {
-#pragma unroll
-    for (int i = 0; i < ST; ++i) {
-      const int r = i * RPI + tid / CH;
-      *(uint4*)(tile[to] + r * ROW + (((tid % CH) ^ (r & (CH - 1))) << 4)) = st[i];
-    }
-    lse_of[to][wave][lane] = st_lse == -INFINITY ? INFINITY : st_lse * kLog2e;
-    pos_of[to][wave][lane] = st_pos;
-  };
-
-  if (t0 < t1) {
-    fetch();
-    put((int)(t0 & 1));
-  }
-  for (int64_t t = t0; t < t1; ++t) {
-    const int cur = (int)(t & 1);
-    // which of the tile's row blocks see any of the wavefront's keys, and which not all
+  for (int f = 0; f < KB; ++f) sum[f] = 0.f;
+  for (int t = t0; t < t1; ++t) {
+    const int cur = t & 1;
+    // which of the tile's rows see any of the wavefront's keys, and which not all
     const bool real = st_pos != INT32_MIN;
     const uint64_t some = __builtin_amdgcn_ballot_w64(real && st_pos >= k_min);
     const uint64_t hide = __builtin_amdgcn_ballot_w64(real && st_pos < k_max);
     __syncthreads();
-    if (t + 1 < t1) fetch();
-#pragma unroll
-    for (int rb = 0; rb < TILE / 32; ++rb) {
-      if ((uint32_t)(some >> (32 * rb)) == 0) continue;
-      const bool masked = (uint32_t)(hide >> (32 * rb)) != 0;
-      floatx16_t s[KB];
-#pragma unroll
-      for (int f = 0; f < KB; ++f)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[f][i] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) {
-        const int r = rb * 32 + rl;
-        const uint4 qf = *(const uint4*)(tile[cur] + r * ROW + (((2 * ks + hf) ^ (r & (CH - 1))) << 4));
-#pragma unroll
-        for (int f = 0; f < KB; ++f) s[f] = product(qf, kf[f][ks], s[f], TI());
-      }
-      // score i of lane (rl, hf): key rl, row (i / 4) * 8 + hf * 4 + i % 4
-      floatx4_t lr[4];
+    if (t + 1 < t1) fetch(t + 1);
+    // score i of lane (rl, hf) in a row and key block: key rl, row (i / 4) * 8 + hf * 4 + i % 4
+    auto q_chunk = [&](int rb, int ks) -> uint4 {
+      const int r = rb * 32 + rl;
+      return *(const uint4*)(tile[cur] + r * ROW + (((2 * ks + hf) ^ (r & (CH - 1))) << 4));
+    };
+    auto lse_rows = [&](int rb, floatx4_t (&lr)[4]) {
 #pragma unroll
       for (int a = 0; a < 4; ++a)
         lr[a] = *(const floatx4_t*)&lse_of[cur][wave][rb * 32 + a * 8 + hf * 4];
+    };
+    auto term = [&](const floatx16_t& s, const floatx4_t (&lr)[4], int i) {
+      return __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -lr[i >> 2][i & 3]));
+    };
+    if (KB > 1 && some != 0 && hide == 0) {
+      constexpr int RB = TILE / 32, NB = RB * KB, PER = 16 / NKS > 0 ? 16 / NKS : 1;
+      floatx16_t s[2];
+      floatx4_t lr[RB][4];
+      uint4 qf[NKS];
 #pragma unroll
-      for (int f = 0; f < KB; ++f) {
+      for (int ks = 0; ks < NKS; ++ks) qf[ks] = q_chunk(0, ks);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) lse_rows(rb, lr[rb]);
+#pragma unroll
+      for (int j = 0; j <= NB; ++j) {   // products of block j, exponentials of block j - 1
+        float x[2] = {0.f, 0.f};
+        if (j < NB)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[j & 1][i] = 0.f;
+        // a step behind a product: arguments of PER scores, exponentials of the PER before them, the
+        // sum of those before (neither waits for the instruction in front of it)
         float e[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          e[i] = __builtin_amdgcn_exp2f(fmaf(s[f][i], p.scale_log2, -lr[i >> 2][i & 3]));
-        if (masked) {
+        for (int ks = 0; ks < NKS + 2; ++ks) {
+          if (j < NB && ks < NKS) {
+            s[j & 1] = product(qf[ks], kf[j % KB][ks], s[j & 1], TI());
+            if (j % KB == KB - 1 && j / KB + 1 < RB) qf[ks] = q_chunk(j / KB + 1, ks);
+          }
+          if (j > 0) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+              const int a = ks * PER + i, b = a - PER, c = b - PER;
+              if (c >= 0 && c < 16) x[c & 1] += e[c];
+              if (b >= 0 && b < 16) e[b] = __builtin_amdgcn_exp2f(e[b]);
+              if (a < 16) e[a] = fmaf(s[(j - 1) & 1][a], p.scale_log2, -lr[(j - 1) / KB][a >> 2][a & 3]);
+            }
+          }
+          if (j < NB) __builtin_amdgcn_sched_barrier(0);
+        }
+        if (j > 0) sum[(j - 1) % KB] += x[0] + x[1];
+      }
+    } else if (some != 0) {
+#pragma unroll
+      for (int rb = 0; rb < TILE / 32; ++rb) {
+        floatx4_t lr[4];
+        lse_rows(rb, lr);
+        floatx16_t s[KB];
+#pragma unroll
+        for (int f = 0; f < KB; ++f)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[f][i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+          const uint4 qf = q_chunk(rb, ks);
+#pragma unroll
+          for (int f = 0; f < KB; ++f) s[f] = product(qf, kf[f][ks], s[f], TI());
+        }
+#pragma unroll
+        for (int f = 0; f < KB; ++f) {
+          float x[2] = {0.f, 0.f};
 #pragma unroll
           for (int a = 0; a < 4; ++a) {
             const int4 q = *(const int4*)&pos_of[cur][wave][rb * 32 + a * 8 + hf * 4];
-            e[4 * a] = q.x >= kp[f] ? e[4 * a] : 0.f;
-            e[4 * a + 1] = q.y >= kp[f] ? e[4 * a + 1] : 0.f;
-            e[4 * a + 2] = q.z >= kp[f] ? e[4 * a + 2] : 0.f;
-            e[4 * a + 3] = q.w >= kp[f] ? e[4 * a + 3] : 0.f;
-          }
-        }
-        float x = (e[0] + e[1]) + (e[2] + e[3]);
+            const int32_t qp[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int a = 1; a < 4; ++a)
-          x += (e[4 * a] + e[4 * a + 1]) + (e[4 * a + 2] + e[4 * a + 3]);
-        sum[f] += x;
+            for (int i = 0; i < 4; ++i) {
+              const float e = term(s[f], lr, 4 * a + i);
+              x[i & 1] += qp[i] >= kp[f] ? e : 0.f;
+            }
+          }
+          sum[f] += x[0] + x[1];
+        }
       }
     }
     if (t + 1 < t1) put(cur ^ 1);
@@ -298,28 +354,44 @@ __global__ __launch_bounds__(NW * 64, KB == 1 && sizeof(TI) == 2 ? 4 : 2) void k
     const float x = sum[f] + __shfl_xor(sum[f], 32, 64);
     const int key = key0 + f * KEYS + rl;
     if (hf == 0 && key < sq.used) {
-      const int64_t to = sq.k0 + key;
+      const int64_t to = (int64_t)sq.k0 + key;
       if (p.part != nullptr)
         p.part[(int64_t)blockIdx.y * p.total_kv + to] = x;
       else
-        p.weight[to] = p.decay != 0.f ? fmaf(p.weight[to], p.decay, x) : x;
+        p.weight[to] = p.decay != 0.f ? fmaf(old[f], p.decay, x) : x;
     }
   }
 }
 
-// weight <- decay * weight + the parts, in their order.
+// weight <- decay * weight + the parts: four threads a key, each every fourth part in order, then theirs
+// in order.
+constexpr int SUM_KEYS = 64;
 __global__ __launch_bounds__(256) void kv_weight_sum_kernel(const WeightParams p) {
+  __shared__ float sums[4][SUM_KEYS];
   int begin = 0;
-  const int b = find_block(p, blockIdx.x, &begin);
-  if (b < 0) return;
-  const Seq sq = seq_of(p, b);
-  const int key = ((int)blockIdx.x - begin) * p.wg_keys + threadIdx.x;
-  if ((int)threadIdx.x >= p.wg_keys || key >= sq.used) return;
-  const int64_t at = sq.k0 + key;
+  Seq sq;
+  const int per = p.wg_keys / SUM_KEYS;
+  if (find_block(p, blockIdx.x / per, &begin, &sq) < 0) return;
+  const int lane = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+  const int key = ((int)blockIdx.x / per - begin) * p.wg_keys + (int)blockIdx.x % per * SUM_KEYS + lane;
+  const int64_t at = (int64_t)sq.k0 + min(key, sq.used - 1);
   const int n = p.n_ranges * p.n_kv_heads;
+  const float old = quarter == 0 && p.decay != 0.f ? p.weight[at] : 0.f;
   float t = 0.f;
-  for (int i = 0; i < n; ++i) t += p.part[(int64_t)i * p.total_kv + at];
-  p.weight[at] = p.decay != 0.f ? fmaf(p.weight[at], p.decay, t) : t;
+  constexpr int U = 8;   // parts in flight
+  for (int i = quarter; i < n; i += 4 * U) {
+    float x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = i + 4 * u < n ? p.part[(int64_t)(i + 4 * u) * p.total_kv + at] : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) t += x[u];
+  }
+  sums[quarter][lane] = t;
+  __syncthreads();
+  if (quarter == 0 && key < sq.used) {
+    t = ((sums[0][lane] + sums[1][lane]) + sums[2][lane]) + sums[3][lane];
+    p.weight[at] = p.decay != 0.f ? fmaf(old, p.decay, t) : t;
+  }
 }
 
 struct WeightPlan {
@@ -328,6 +400,7 @@ struct WeightPlan {
   int n_ranges;
   size_t bytes;
 };
+constexpr double kStartTiles = 3;
 WeightPlan weight_plan(const cp_shape& s) {
   WeightPlan pl = {};
   const int64_t rows = (s.total_q * (s.n_q_heads / s.n_kv_heads) + s.batch - 1) / s.batch;
@@ -335,9 +408,18 @@ WeightPlan weight_plan(const cp_shape& s) {
   pl.kb = tiles <= 1 || s.dtype == CP_FP32 ? 1 : 2;
   const int wg_keys = NW * pl.kb * KEYS;
   pl.blocks = s.total_kv / wg_keys + s.batch;
-  // ranges of the rows until there are eight workgroups per CU, of four tiles at least
+  // Ranges of the rows: as many as make the least of (rounds of workgroups, two a CU, and one for the
+  // tail) times (tiles of one, and what it costs to begin). Which of them see nothing is not known here.
   int64_t n = 1;
-  while (n < 64 && pl.blocks * s.n_kv_heads * n < 2048 && tiles >= n * 2 * 4) n *= 2;
+  double least = 1e30;
+  for (int64_t i = 1; i <= 128 && i <= tiles; ++i) {
+    const double cost = ((double)(pl.blocks * s.n_kv_heads * i) / 512 + 1) *
+                        (kStartTiles + (double)((tiles + i - 1) / i));
+    if (cost < least) {
+      least = cost;
+      n = i;
+    }
+  }
   pl.n_ranges = (int)n;
   const int64_t parts = n * s.n_kv_heads;
   pl.bytes = parts > 1 ? (size_t)parts * s.total_kv * 4 : 0;
@@ -370,7 +452,8 @@ extern "C" int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int
     return CP_ERR_NULL;
   if (!aligned16(q) || !aligned16(k_cache)) return CP_ERR_ALIGN;
   if (s.total_kv == 0) return CP_OK;
-  if (s.total_kv > INT32_MAX - 256) return CP_ERR_SHAPE;   // key indices in 31 bits
+  // key indices and rows in 31 bits
+  if (s.total_kv > INT32_MAX - 256 || s.total_q * s.n_q_heads > INT32_MAX - TILE) return CP_ERR_SHAPE;
   const WeightPlan pl = weight_plan(s);
   if (pl.bytes > 0 && (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 ||
                        workspace_bytes < pl.bytes))
@@ -390,21 +473,25 @@ extern "C" int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int
   p.decay = decay;
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid((unsigned)pl.blocks, (unsigned)parts);
-#define CP_WEIGHT(TI, D, KB) \
-  hipLaunchKernelGGL((kv_weight_kernel<TI, D, KB>), grid, dim3(NW * 64), 0, st, p)
+#define CP_WEIGHT(TI, D, KB)                                                                        \
+  if (s.n_kv_heads == 1)                                                                            \
+    hipLaunchKernelGGL((kv_weight_kernel<TI, D, KB, true>), grid, dim3(NW * 64), 0, st, p);          \
+  else                                                                                              \
+    hipLaunchKernelGGL((kv_weight_kernel<TI, D, KB, false>), grid, dim3(NW * 64), 0, st, p)
   if (s.dtype == CP_FP32) {
-    if (s.head_dim == 64) CP_WEIGHT(float, 64, 1);
-    else CP_WEIGHT(float, 128, 1);
+    if (s.head_dim == 64) { CP_WEIGHT(float, 64, 1); }
+    else { CP_WEIGHT(float, 128, 1); }
   } else if (s.head_dim == 64) {
-    if (pl.kb == 1) CP_WEIGHT(bf16_t, 64, 1);
-    else CP_WEIGHT(bf16_t, 64, 2);
+    if (pl.kb == 1) { CP_WEIGHT(bf16_t, 64, 1); }
+    else { CP_WEIGHT(bf16_t, 64, 2); }
   } else {
-    if (pl.kb == 1) CP_WEIGHT(bf16_t, 128, 1);
-    else CP_WEIGHT(bf16_t, 128, 2);
+    if (pl.kb == 1) { CP_WEIGHT(bf16_t, 128, 1); }
+    else { CP_WEIGHT(bf16_t, 128, 2); }
   }
 #undef CP_WEIGHT
   if (check_launch() != CP_OK) return CP_ERR_LAUNCH;
   if (p.part == nullptr) return CP_OK;
-  hipLaunchKernelGGL(kv_weight_sum_kernel, dim3((unsigned)pl.blocks), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(kv_weight_sum_kernel, dim3((unsigned)(pl.blocks * (p.wg_keys / SUM_KEYS))), dim3(256), 0,
+                     st, p);
   return check_launch();
 }
