@@ -52,83 +52,138 @@ struct TreeParams {
   float* part_ml;          // [2 * n_wg][row block][2]: running maximum (log2 domain), sum
   int64_t total_q, total_kv;
   int32_t batch, words, n_q_heads, n_kv_heads, group;
-  int32_t n_wg, min_share;
+  int32_t n_wg, log2_wg;   // workgroups among which the line is dealt out, a power of two
+  int32_t min_share;
   float scale_log2;
 };
 
 // What a sequence holds. Boundaries that contradict each other or the totals (they are read on the
 // device, where nothing can be refused) are cut to what is there.
 struct TreeSeq {
-  int64_t q0, k0;      // first node, first cache slot
-  int32_t n, used;     // nodes, tokens in the cache
-  int64_t spans, tiles;
+  int32_t q0, n, k0, used;   // first node, nodes, first cache slot, tokens in the cache
+  int32_t spans, tiles;      // row blocks of a KV head, tiles of each
+  __device__ __forceinline__ TreeSeq of_lane(int l) const {
+    TreeSeq r;
+    r.q0 = __builtin_amdgcn_readlane(q0, l);
+    r.n = __builtin_amdgcn_readlane(n, l);
+    r.k0 = __builtin_amdgcn_readlane(k0, l);
+    r.used = __builtin_amdgcn_readlane(used, l);
+    r.spans = __builtin_amdgcn_readlane(spans, l);
+    r.tiles = __builtin_amdgcn_readlane(tiles, l);
+    return r;
+  }
+  __device__ __forceinline__ int cached_subs() const { return (used + SUB - 1) / SUB; }
 };
-// RM rows of a row block, SPT sub-tiles of a tile
-template <int RM, int SPT>
-__device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
-  TreeSeq s;
-  s.q0 = clamp64(p.cu_q[b], 0, p.total_q);
-  s.n = (int32_t)(clamp64(p.cu_q[b + 1], s.q0, p.total_q) - s.q0);
-  s.k0 = clamp64(p.cu_kv[b], 0, p.total_kv);
-  const int64_t room = clamp64(p.cu_kv[b + 1], s.k0, p.total_kv) - s.k0;
-  s.used = (int32_t)(p.used != nullptr ? clamp64(p.used[b], 0, room) : room);
-  s.spans = ((int64_t)s.n * p.group + RM - 1) / RM;
-  const int64_t subs = (s.used + SUB - 1) / SUB + (p.k_new != nullptr ? (s.n + SUB - 1) / SUB : 0);
-  s.tiles = subs > 0 ? (subs + SPT - 1) / SPT : 1;   // (nothing to see: one tile, empty)
-  return s;
+
+__device__ __forceinline__ int64_t wave_scan64(int64_t x) {   // of numbers from 0 to 2^48
+  const int lo = wave_scan((int)(x & 0xffffff)), hi = wave_scan((int)(x >> 24));
+  return ((int64_t)hi << 24) + lo;
+}
+__device__ __forceinline__ int64_t readlane64(int64_t x, int l) {
+  return ((int64_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)x, l);
+}
+__device__ __forceinline__ uint32_t div64(uint64_t a, uint32_t b) {   // quotient in 32 bits
+  return (a >> 32) == 0 ? (uint32_t)a / b : (uint32_t)(a / b);
 }
 
-__device__ __forceinline__ int64_t wave_sum64(int64_t x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-  return x;
-}
-
-// Tiles of one KV head.
+// The line of all tiles: KV heads, in each the sequences, in each the row blocks (RM rows), in each the
+// tiles (SPT sub-tiles). Up to 64 sequences are described by one round trip, a lane each; of more, the
+// lanes hold 64 at a time.
 template <int RM, int SPT>
-__device__ __forceinline__ int64_t tree_total(const TreeParams& p) {
-  const int lane = threadIdx.x & 63;
-  int64_t sum = 0;
-  for (int b = lane; b < p.batch; b += 64) {
-    const TreeSeq s = tree_seq<RM, SPT>(p, b);
-    sum += s.spans * s.tiles;
+struct TreeLine {
+  const TreeParams& p;
+  TreeSeq mine;
+  int64_t end;        // tiles of the sequences up to the lane's, of those held
+  int held;           // first of the sequences held
+  int64_t head_tiles, share;
+
+  __device__ __forceinline__ void hold(int b0) {
+    held = b0;
+    const int b = min(b0 + (int)(threadIdx.x & 63), p.batch - 1);
+    const int32_t a0 = p.cu_q[b], a1 = p.cu_q[b + 1], c0 = p.cu_kv[b], c1 = p.cu_kv[b + 1];
+    const int32_t u = p.used != nullptr ? p.used[b] : INT32_MAX;
+    mine.q0 = (int32_t)clamp64(a0, 0, p.total_q);
+    mine.n = (int32_t)clamp64(a1, mine.q0, p.total_q) - mine.q0;
+    mine.k0 = (int32_t)clamp64(c0, 0, p.total_kv);
+    mine.used = (int32_t)clamp64(u, 0, clamp64(c1, mine.k0, p.total_kv) - mine.k0);
+    mine.spans = (mine.n * p.group + RM - 1) / RM;   // (rows of a KV head in 31 bits: the host checks)
+    const int subs = mine.cached_subs() + (p.k_new != nullptr ? (mine.n + SUB - 1) / SUB : 0);
+    mine.tiles = subs > 0 ? (subs + SPT - 1) / SPT : 1;   // (nothing to see: one tile, empty)
+    end = wave_scan64(b0 + (int)(threadIdx.x & 63) < p.batch ? (int64_t)mine.spans * mine.tiles : 0);
   }
-  return wave_sum64(sum);
-}
-
-// The sequence that tile u (of one KV head) belongs to, and the tile where it begins.
-template <int RM, int SPT>
-__device__ __forceinline__ int tree_find(const TreeParams& p, int64_t u, int64_t* begin) {
-  const int lane = threadIdx.x & 63;
-  int64_t base = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    int64_t c = 0;
-    if (b0 + lane < p.batch) {
-      const TreeSeq s = tree_seq<RM, SPT>(p, b0 + lane);
-      c = s.spans * s.tiles;
+  __device__ __forceinline__ explicit TreeLine(const TreeParams& params) : p(params) {
+    head_tiles = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      hold(b0);
+      head_tiles += readlane64(end, 63);
     }
-    int64_t end = c;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t y = __shfl_up(end, o, 64);
-      if (lane >= o) end += y;
-    }
-    const uint64_t behind = __builtin_amdgcn_ballot_w64(base + end > u);
-    if (behind != 0) {
-      const int l = __builtin_ctzll(behind);
-      *begin = base + __shfl(end - c, l, 64);
-      return b0 + l;
-    }
-    base += __shfl(end, 63, 64);
+    const int64_t all = head_tiles * p.n_kv_heads;
+    share = (all + p.n_wg - 1) >> p.log2_wg;
+    if (share < p.min_share) share = p.min_share;
   }
-  *begin = base;
-  return -1;
-}
+  // The sequence of tile u of a KV head (-1: behind the last), and the tile where it begins.
+  __device__ __forceinline__ int find(int64_t u, int64_t* begin, TreeSeq* sq) {
+    int64_t base = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      if (b0 != held) hold(b0);
+      const uint64_t behind = __builtin_amdgcn_ballot_w64(base + end > u);
+      if (behind != 0) {
+        const int l = __builtin_ctzll(behind);
+        *sq = mine.of_lane(l);
+        *begin = base + readlane64(end, l) - (int64_t)sq->spans * sq->tiles;
+        return b0 + l;
+      }
+      base += readlane64(end, 63);
+    }
+    return -1;
+  }
+  // The sequence that node t belongs to (-1: behind the last tree), and the tiles before it.
+  __device__ __forceinline__ int find_node(int t, int64_t* begin, TreeSeq* sq) {
+    int64_t base = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      if (b0 != held) hold(b0);
+      const bool in = b0 + (int)(threadIdx.x & 63) < p.batch;
+      const uint64_t hit = __builtin_amdgcn_ballot_w64(in && t >= mine.q0 && t < mine.q0 + mine.n);
+      if (hit != 0) {
+        const int l = __builtin_ctzll(hit);
+        *sq = mine.of_lane(l);
+        *begin = base + readlane64(end, l) - (int64_t)sq->spans * sq->tiles;
+        return b0 + l;
+      }
+      base += readlane64(end, 63);
+    }
+    return -1;
+  }
+};
 
-// A workgroup's share of the line: as many tiles for each, `min_share` at least.
-__device__ __forceinline__ int64_t tree_share(const TreeParams& p, int64_t all) {
-  const int64_t s = (all + p.n_wg - 1) / p.n_wg;
-  return s < p.min_share ? p.min_share : s;
+// A workgroup's share of a span: tiles [t0, t1) of row block `span` of KV head kvh of a sequence.
+struct TreePiece {
+  TreeSeq sq;
+  int kvh, span, t0, t1;
+  int n_cached, n_subs;
+  bool whole;        // the span is all in this piece: its result goes to the output
+  int slot;          // otherwise: where the part goes
+};
+template <int RM, int SPT>
+__device__ __forceinline__ bool tree_piece(TreeLine<RM, SPT>& line, int64_t u, int64_t u_end, TreePiece* x) {
+  int64_t v = u, begin;
+  x->kvh = 0;
+  while (v >= line.head_tiles) {
+    v -= line.head_tiles;
+    ++x->kvh;
+  }
+  if (line.find(v, &begin, &x->sq) < 0) return false;
+  const int64_t in = v - begin;
+  x->span = (int)div64((uint64_t)in, (uint32_t)x->sq.tiles);
+  x->t0 = (int)(in - (int64_t)x->span * x->sq.tiles);
+  x->t1 = (int)min<int64_t>(x->sq.tiles, x->t0 + (u_end - u));
+  x->n_cached = x->sq.cached_subs();
+  x->n_subs = x->n_cached + (line.p.k_new != nullptr ? (x->sq.n + SUB - 1) / SUB : 0);
+  x->whole = x->t0 == 0 && x->t1 == x->sq.tiles;
+  // a share has at most one part that ends a span and one that begins one
+  x->slot = 2 * (int)blockIdx.x + (x->t0 == 0 ? 1 : 0);
+  return true;
 }
 
 // ---------------------------------------------------------------------------
@@ -230,40 +285,31 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rl = lane & 31, hf = lane >> 5;   // row (N side) or key / channel (M side), half
-  const int64_t head_tiles = tree_total<F::RM, F::SPT>(p);
-  const int64_t all = head_tiles * p.n_kv_heads;
-  const int64_t share = tree_share(p, all);
-  int64_t u = blockIdx.x * share;
-  const int64_t u_end = min(all, u + share);
+  TreeLine<F::RM, F::SPT> line(p);
+  int64_t u = blockIdx.x * line.share;
+  const int64_t u_end = min(line.head_tiles * p.n_kv_heads, u + line.share);
   const int64_t tok_q = (int64_t)p.n_q_heads * D, tok_kv = (int64_t)p.n_kv_heads * D;
 
   while (u < u_end) {
-    const int kvh = (int)(u / head_tiles);
-    int64_t begin;
-    const int b = tree_find<F::RM, F::SPT>(p, u - kvh * head_tiles, &begin);
-    if (b < 0) break;
-    const TreeSeq sq = tree_seq<F::RM, F::SPT>(p, b);
-    const int64_t in = u - kvh * head_tiles - begin;
-    const int64_t span = in / sq.tiles;
-    const int t0 = (int)(in - span * sq.tiles);
-    const int t1 = (int)min<int64_t>(sq.tiles, t0 + (u_end - u));
-    const int n_cached = (sq.used + SUB - 1) / SUB;
-    const int n_subs = n_cached + (p.k_new != nullptr ? (sq.n + SUB - 1) / SUB : 0);
-    const int64_t n_rows = (int64_t)sq.n * p.group;
+    TreePiece pc;
+    if (!tree_piece(line, u, u_end, &pc)) break;
+    const TreeSeq& sq = pc.sq;
+    const int kvh = pc.kvh, t0 = pc.t0, t1 = pc.t1, n_cached = pc.n_cached, n_subs = pc.n_subs;
+    const int n_rows = sq.n * p.group;
 
     // ---- the wavefront's rows ----
-    int64_t row[C];        // within (sequence, KV head)
-    int64_t node[C];       // of all nodes; -1: a row behind the last one
+    int row[C];            // within (sequence, KV head)
+    int node[C];           // of all nodes; -1: a row behind the last one
     int32_t qp[C];
     uint4 qf[C][NKS];      // lane (rl, hf): 16-byte chunk 2 ks + hf of row rl
     int32_t q_min = INT32_MAX, q_max = INT32_MIN;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      row[c] = span * F::RM + (KS ? 0 : wave * F::RW) + c * 32 + rl;
+      row[c] = pc.span * F::RM + (KS ? 0 : wave * F::RW) + c * 32 + rl;
       const bool ok = row[c] < n_rows;
-      const int64_t nd = ok ? row[c] / p.group : 0;
+      const int nd = ok ? (uint32_t)row[c] / (uint32_t)p.group : 0;
       node[c] = ok ? sq.q0 + nd : -1;
-      const int head = kvh * p.group + (ok ? (int)(row[c] - nd * p.group) : 0);
+      const int head = kvh * p.group + (ok ? row[c] - nd * p.group : 0);
       const uint4* src = (const uint4*)((const TI*)p.q + (ok ? node[c] : 0) * tok_q + head * D) + hf;
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks) {
@@ -300,7 +346,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
       const bool own = st >= n_cached;
       const int first = (own ? st - n_cached : st) * SUB;
       const int last = min(SUB, (own ? sq.n : sq.used) - first) - 1;
-      const int64_t base = (own ? sq.q0 : sq.k0) + first;
+      const int64_t base = (int64_t)(own ? sq.q0 : sq.k0) + first;
       const TI* kt = (const TI*)(own ? p.k_new : p.k) + base * tok_kv + kvh * D;
       const TI* vt = (const TI*)(own ? p.v_new : p.v) + base * tok_kv + kvh * D;
       constexpr int RPI = 64 / T::CH;          // rows of a request
@@ -366,7 +412,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
             const int word = (st - n_cached) >> 1;
             see = 0;
             if (node[c] >= 0 && word < p.words)
-              see = (uint32_t)(p.mask[node[c] * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
+              see = (uint32_t)(p.mask[(int64_t)node[c] * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
           }
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -543,18 +589,16 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
     for (int c = 0; c < C; ++c) l_run[c] += xor32(l_run[c]);
 
     // ---- the span's result, or this share's part of it ----
-    const bool whole = t0 == 0 && t1 == sq.tiles;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (t0 == 0 ? 1 : 0);
-    auto write = [&](int64_t r, int in_block, float m, float l, int ch, floatx4_t o4) {
+    auto write = [&](int r, int in_block, float m, float l, int ch, floatx4_t o4) {
       if (r >= n_rows) return;
-      if (whole) {
-        const int64_t nd = r / p.group;
-        const int64_t at = (sq.q0 + nd) * p.n_q_heads + kvh * p.group + (r - nd * p.group);
+      if (pc.whole) {
+        const int nd = (uint32_t)r / (uint32_t)p.group;
+        const int64_t at = (int64_t)(sq.q0 + nd) * p.n_q_heads + kvh * p.group + (r - nd * p.group);
         const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;   // (a NaN stays one)
         store4<TO>((TO*)p.out + at * D + ch, o4 * inv);
         if (ch == 0) p.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
       } else {
-        const int64_t at = slot * F::RM + in_block;
+        const int64_t at = (int64_t)pc.slot * F::RM + in_block;
         *(floatx4_t*)(p.part_o + at * D + ch) = o4;
         if (ch == 0) {
           p.part_ml[at * 2] = m;
@@ -599,7 +643,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
           l = fmaf(lw, f, l);
           o4 += x * f;
         }
-        write(span * F::RM + r, r, m, l, ch, o4);
+        write(pc.span * F::RM + r, r, m, l, ch, o4);
       }
       __syncthreads();
     } else {
@@ -617,61 +661,72 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
   }
 }
 
-// Joins the parts of the spans that fell into several shares: a wavefront per row.
+// Joins the parts of the spans that fell into several shares, a wavefront per row: lane l knows the
+// maximum and sum of part l, and the rows of eight parts are in flight at a time.
 template <int D, int RM, int SPT, typename TO>
 __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
-  constexpr int V = D / 64;
+  constexpr int V = D / 64, U = 8;
+  typedef float vec_t __attribute__((ext_vector_type(V)));
   const int lane = threadIdx.x & 63;
-  const int64_t all_rows = p.total_q * p.n_q_heads;
-  const int64_t idx = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (idx >= all_rows) return;
-  const int64_t node = idx / p.n_q_heads;
-  const int head = (int)(idx - node * p.n_q_heads), kvh = head / p.group;
-  // the sequence of this node and the tiles before it
-  int64_t before = 0, total = 0;
-  int b = -1;
-  for (int b0 = 0; b0 < p.batch; b0 += 64) {
-    int64_t c = 0;
-    bool mine = false;
-    if (b0 + lane < p.batch) {
-      const TreeSeq s = tree_seq<RM, SPT>(p, b0 + lane);
-      c = s.spans * s.tiles;
-      mine = node >= s.q0 && node < s.q0 + s.n;
+  const int64_t idx = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (idx >= p.total_q * p.n_q_heads) return;
+  const int node = (uint32_t)idx / (uint32_t)p.n_q_heads;
+  const int head = (int)idx - node * p.n_q_heads, kvh = (uint32_t)head / (uint32_t)p.group;
+  TreeLine<RM, SPT> line(p);
+  TreeSeq sq;
+  int64_t before;
+  if (line.find_node(node, &before, &sq) < 0) return;   // behind the last tree
+  const int row = (node - sq.q0) * p.group + (head - kvh * p.group);
+  const int span = row / RM;
+  const int64_t a = kvh * line.head_tiles + before + (int64_t)span * sq.tiles;
+  const int w0 = (int)div64((uint64_t)a, (uint32_t)line.share);
+  const int n = (int)div64((uint64_t)(a + sq.tiles - 1), (uint32_t)line.share) - w0 + 1;
+  if (n == 1) return;
+  // (the first part begins the span)
+  auto at = [&](int k) { return (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * RM + (row - span * RM); };
+  float m = -INFINITY, l = 0.f;
+  vec_t o = {};
+  for (int k0 = 0; k0 < n; k0 += 64) {
+    const int cnt = min(64, n - k0);
+    float mw = -INFINITY, lw = 0.f;
+    if (lane < cnt) {
+      const float2 x = *(const float2*)(p.part_ml + at(k0 + lane) * 2);
+      mw = x.x;
+      lw = x.y;
     }
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(mine);
-    if (b < 0 && hit != 0) {
-      const int l = __builtin_ctzll(hit);
-      b = b0 + l;
-      before = total + wave_sum64(lane < l ? c : 0);
-    }
-    total += wave_sum64(c);
-  }
-  if (b < 0) return;   // behind the last tree
-  const TreeSeq s = tree_seq<RM, SPT>(p, b);
-  const int64_t row = (node - s.q0) * p.group + (head - kvh * p.group);
-  const int64_t span = row / RM;
-  const int64_t a = kvh * total + before + span * s.tiles, e = a + s.tiles;
-  const int64_t share = tree_share(p, total * p.n_kv_heads);
-  const int64_t w0 = a / share, w1 = (e - 1) / share;
-  if (w0 == w1) return;
-  float m = -INFINITY, l = 0.f, o[V];
+    vec_t x[U];
+    auto rows = [&](int k) {
 #pragma unroll
-  for (int i = 0; i < V; ++i) o[i] = 0.f;
-  for (int64_t w = w0; w <= w1; ++w) {
-    const int64_t at = (2 * w + (w == w0 ? 1 : 0)) * RM + (row - span * RM);
-    const float mw = p.part_ml[at * 2], lw = p.part_ml[at * 2 + 1];
-    if (lw == 0.f) continue;
-    const float mn = fmaxf(m, mw);
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-    const float fw = __builtin_amdgcn_exp2f(mw - mn);
+      for (int u = 0; u < U; ++u) x[u] = *(const vec_t*)(p.part_o + at(k0 + min(k + u, cnt - 1)) * D + lane * V);
+    };
+    rows(0);
+    float top = mw;
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
+    const float mn = fmaxf(m, top);
+    const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    // (a part that saw nothing has weight 0; one that saw a NaN alone has no maximum and that sum)
+    const float f = lw == 0.f ? 0.f : mw == -INFINITY ? lw : __builtin_amdgcn_exp2f(mw - mn);
+    float sum = lw * f;
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s, 64);
+    l = fmaf(l, old, sum);
     m = mn;
-    l = fmaf(l, f, lw * fw);
+    o *= old;
+    for (int k = 0; k < cnt; k += U) {
+      if (k > 0) rows(k);
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = fmaf(o[i], f, p.part_o[at * D + lane * V + i] * fw);
+      for (int u = 0; u < U; ++u) {
+        const float fu = k + u < cnt ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(
+                                           __builtin_bit_cast(int, f), k + u)) : 0.f;
+        if (k + u < cnt) o += x[u] * fu;
+      }
+    }
   }
   const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  o *= inv;
 #pragma unroll
-  for (int i = 0; i < V; ++i) ((TO*)p.out)[idx * D + lane * V + i] = from_float<TO>(o[i] * inv);
+  for (int i = 0; i < V; ++i) ((TO*)p.out)[idx * D + lane * V + i] = from_float<TO>(o[i]);
   if (lane == 0) p.lse[idx] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
@@ -745,7 +800,7 @@ inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 enum TreeForm { kFew32, kFew64, kMany };
 struct TreePlan {
   TreeForm form;
-  int rm, spt, n_wg, min_share;
+  int rm, spt, n_wg, log2_wg, min_share;
   size_t o_bytes, ml_bytes;
 };
 constexpr int kManyWaves = 8;
@@ -763,7 +818,8 @@ TreePlan tree_plan(const cp_shape& s) {
   const int64_t tiles = (s.total_kv + s.total_q) / (SUB * pl.spt) + 2 * (int64_t)s.batch;
   const int64_t most = pl.form == kMany ? 256 : 512;
   const int64_t any = spans > most || tiles > most ? most : spans * tiles * s.n_kv_heads;
-  pl.n_wg = (int)(any < most ? any : most);
+  while ((1 << pl.log2_wg) < any && (1 << pl.log2_wg) < most) ++pl.log2_wg;
+  pl.n_wg = 1 << pl.log2_wg;
   pl.o_bytes = round256((size_t)2 * pl.n_wg * pl.rm * s.head_dim * 4);
   pl.ml_bytes = round256((size_t)2 * pl.n_wg * pl.rm * 2 * 4);
   return pl;
@@ -860,7 +916,7 @@ int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
     return CP_ERR_ALIGN;
   if (s.total_q == 0) return CP_OK;
   // rows of the merge's grid, nodes and tokens of a sequence with their sub-tiles are kept in 31 bits
-  if (s.total_q * s.n_q_heads > INT32_MAX || s.total_kv > INT32_MAX - SUB || s.batch > (1 << 24))
+  if (s.total_q * s.n_q_heads > INT32_MAX - 1024 || s.total_kv > INT32_MAX - 1024 || s.batch > (1 << 24))
     return CP_ERR_SHAPE;
   const TreePlan pl = tree_plan(s);
   if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 ||
@@ -875,7 +931,7 @@ int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
   p.part_ml = (float*)((char*)workspace + pl.o_bytes);
   p.total_q = s.total_q; p.total_kv = s.total_kv; p.batch = s.batch;
   p.n_q_heads = s.n_q_heads; p.n_kv_heads = s.n_kv_heads; p.group = s.n_q_heads / s.n_kv_heads;
-  p.n_wg = pl.n_wg; p.min_share = pl.min_share;
+  p.n_wg = pl.n_wg; p.log2_wg = pl.log2_wg; p.min_share = pl.min_share;
   p.scale_log2 = (s.softmax_scale > 0.f ? s.softmax_scale : 1.0f / sqrtf((float)s.head_dim)) * kLog2e;
   hipStream_t st = (hipStream_t)stream;
   const bool f32_out = out_dtype == CP_FP32;
