@@ -252,8 +252,8 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t x) {
   if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
   return x;
 }
-__device__ __forceinline__ bool any_not_finite(uint32_t x) {
-  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+__device__ __forceinline__ uint32_t any_not_finite(uint32_t x) {   // 1 or 0, without a branch
+  return (uint32_t)((x & 0x7f80u) == 0x7f80u) | (uint32_t)((x & 0x7f800000u) == 0x7f800000u);
 }
 
 // KS: the wavefronts of a workgroup hold the same 32 C rows and take turns at the sub-tiles (few
@@ -428,8 +428,8 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
             odd_v |= (x.x & 0x7f800000u) == 0x7f800000u || (x.y & 0x7f800000u) == 0x7f800000u ||
                      (x.z & 0x7f800000u) == 0x7f800000u || (x.w & 0x7f800000u) == 0x7f800000u;
           else
-            odd_v |= any_not_finite(x.x) || any_not_finite(x.y) || any_not_finite(x.z) ||
-                     any_not_finite(x.w);
+            odd_v |= (any_not_finite(x.x) | any_not_finite(x.y) | any_not_finite(x.z) |
+                      any_not_finite(x.w)) != 0;
         }
         odd_v = __builtin_amdgcn_ballot_w64(odd_v) != 0;
       }
@@ -661,6 +661,424 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
   }
 }
 
+// ---------------------------------------------------------------------------
+// Many rows (bf16): eight wavefronts with 32 rows each, a tile of 64 keys for all of them.
+//
+// Bound by the matrix pipe and, about as much, by the LDS reads that feed it (a fragment serves 32 rows).
+// A step works on three sub-tiles: the products S^T of the next one and O^T of the one before are issued
+// between the softmax arithmetic of the current one, which needs neither. The reference that the
+// exponentials are taken against is raised only when a score exceeds it by 2^8 (O and the sum are
+// rescaled then): they cancel in O / l, and what is rounded has the same relative error at any scale.
+// A tile travels through registers into one of three LDS buffers: one holds the values of the
+// sub-tile before, one the current tile, and one is being filled; one barrier a tile.
+// ---------------------------------------------------------------------------
+constexpr int MANY_WAVES = 8;
+constexpr int MANY_ROWS = 32 * MANY_WAVES;
+constexpr float kSlack = 8.f;
+
+template <int J>
+struct IntC {
+  static constexpr int value = J;
+};
+// max over the two halves of a wavefront that share a row (inline assembly: through the builtin the
+// compiler takes the two results of a swap of equal operands for equal; the s_nop covers the wait states
+// that a lane swap needs after a vector write of its operands)
+__device__ __forceinline__ float halves_max(float x) {
+  float a = x, b = x;
+  asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+  return fmaxf(a, b);
+}
+// Keeps the computation of x where it is in the instruction stream.
+__device__ __forceinline__ void pin(float& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin(u32x4_t& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void pin(floatx16_t& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  bf16x2_t t;
+  t[0] = static_cast<bf16_t>(a);
+  t[1] = static_cast<bf16_t>(b);
+  return __builtin_bit_cast(uint32_t, t);
+}
+
+template <int D>
+struct ManyTile {
+  using T = SubTile<bf16_t, D>;
+  static constexpr int KEYS = 2 * SUB;
+  static constexpr int V_OFF = KEYS * T::ROW;
+  static constexpr int POS_OFF = 2 * KEYS * T::ROW;
+  static constexpr int BYTES = POS_OFF + KEYS * 4;
+  static constexpr int ZERO_OFF = 3 * BYTES;           // a sub-tile's worth of V, zeros
+  static constexpr int SMEM = ZERO_OFF + SUB * T::ROW;
+};
+
+template <int D, int TERMS, typename TO>
+__global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreeParams p) {
+  using M = ManyTile<D>;
+  using T = SubTile<bf16_t, D>;
+  constexpr int NKS = D / 16, NCB = D / 32, NVF = 2 * NCB;
+  constexpr int THREADS = MANY_WAVES * 64, RPI = THREADS / T::CH, CPT = M::KEYS / RPI;
+  static_assert(NKS == NVF, "a V^T fragment takes the registers of a K fragment");
+  extern __shared__ __align__(16) char smem[];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rl = lane & 31, hf = lane >> 5;
+  for (int i = tid * 16; i < SUB * T::ROW; i += THREADS * 16)
+    *(uint4*)(smem + M::ZERO_OFF + i) = make_uint4(0, 0, 0, 0);
+  int64_t u = 0, u_end = 1;
+  const int64_t tok_q = (int64_t)p.n_q_heads * D, tok_kv = (int64_t)p.n_kv_heads * D;
+  // LDS offsets of this lane inside a sub-tile: K fragment chunk 2 ks + hf of row rl; V^T fragments
+  // (cb, kb): channels of block cb, keys kb*16 + x*8 + hf*4 + 0..3 (v_perm of a row depends on vj alone).
+  // Chunks are permuted by exclusive-or, and so are the offsets of the others (ks * 32, cb * 64).
+  const int koff = rl * T::ROW + ((hf ^ T::k_perm(rl)) << 4);
+  const int vj = (lane & 15) >> 2, vq = lane & 3, vg = (lane >> 4) & 1;
+  const int voff = (hf * 4 + vj) * T::ROW + (((vg * 2 + (vq >> 1)) ^ T::v_perm(vj)) << 4) + (vq & 1) * 8;
+  static_assert(M::BYTES % 256 == 0 && M::V_OFF % 256 == 0 && SUB * T::ROW % 256 == 0, "as the permutation asks");
+
+  for (bool first = true; first || u < u_end; first = false) {
+    TreePiece pc;
+    {
+      // (described anew for every piece: the lanes' sequences would take registers all along)
+      TreeLine<MANY_ROWS, 2> line(p);
+      if (first) {
+        u = blockIdx.x * line.share;
+        u_end = min(line.head_tiles * p.n_kv_heads, u + line.share);
+        if (u >= u_end) return;
+      }
+      if (!tree_piece(line, u, u_end, &pc)) return;
+    }
+    const TreeSeq& sq = pc.sq;
+    const int kvh = pc.kvh, n_cached = pc.n_cached, n_subs = pc.n_subs;
+    const int n_rows = sq.n * p.group;
+    const int row = pc.span * MANY_ROWS + wave * 32 + rl;
+    const bool ok = row < n_rows;
+    const int nd = ok ? (uint32_t)row / (uint32_t)p.group : 0;
+    const int node = sq.q0 + nd;
+    const int head = kvh * p.group + (ok ? row - nd * p.group : 0);
+
+    // ---- a tile on its way: K and V rows by 16-byte chunks, positions of the cached ones ----
+    const bf16_t* const kc = (const bf16_t*)p.k + sq.k0 * tok_kv + kvh * D;
+    const bf16_t* const vc = (const bf16_t*)p.v + sq.k0 * tok_kv + kvh * D;
+    const bf16_t* const kt = (const bf16_t*)p.k_new + sq.q0 * tok_kv + kvh * D;
+    const bf16_t* const vt = (const bf16_t*)p.v_new + sq.q0 * tok_kv + kvh * D;
+    const bool has_tree = p.k_new != nullptr;
+    static_assert(CPT <= 2, "chunks of a lane");
+    uint4 st_k0, st_k1, st_v0, st_v1;   // (scalars: an array of these ends up in memory)
+    int32_t st_pos = 0;
+    auto fetch_row = [&](int idx, uint4& k, uint4& v) __attribute__((always_inline)) {
+      // (keys behind the last of either kind repeat it, and are masked by their index; a choice between
+      // values, since one between the variables would put them into memory)
+      const bool own = has_tree && idx >= n_cached * SUB;
+      const int key = own ? min(idx - n_cached * SUB, sq.n - 1) : min(idx, sq.used - 1);
+      const int64_t off = key * tok_kv;
+      const bf16_t* const kr = own ? kt + off : kc + off;
+      const bf16_t* const vr = own ? vt + off : vc + off;
+      k = ((const uint4*)kr)[tid % T::CH];
+      v = ((const uint4*)vr)[tid % T::CH];
+    };
+    auto fetch = [&](int t) __attribute__((always_inline)) {
+      fetch_row(t * M::KEYS + tid / T::CH, st_k0, st_v0);
+      if constexpr (CPT > 1) fetch_row(t * M::KEYS + RPI + tid / T::CH, st_k1, st_v1);
+      if (tid < M::KEYS) {
+        const int idx = t * M::KEYS + tid;
+        st_pos = idx < sq.used ? p.kv_pos[sq.k0 + idx] : CP_POS_PAD_KV;
+      }
+    };
+    auto put_row = [&](char* buf, int r, const uint4& k, const uint4& v) __attribute__((always_inline)) {
+      const int c = tid % T::CH;
+      *(uint4*)(buf + r * T::ROW + ((c ^ T::k_perm(r & 31)) << 4)) = k;
+      *(uint4*)(buf + M::V_OFF + r * T::ROW + ((c ^ T::v_perm(r & 31)) << 4)) = v;
+    };
+    auto put = [&](char* buf) __attribute__((always_inline)) {
+      put_row(buf, tid / T::CH, st_k0, st_v0);
+      if constexpr (CPT > 1) put_row(buf, RPI + tid / T::CH, st_k1, st_v1);
+      if (tid < M::KEYS) *(int32_t*)(buf + M::POS_OFF + tid * 4) = st_pos;
+    };
+    if (n_subs > 0) fetch(pc.t0);
+
+    uint4 qf[NKS];
+    const uint4* const q_src = (const uint4*)((const bf16_t*)p.q + node * tok_q + head * D) + hf;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      qf[ks] = make_uint4(0, 0, 0, 0);
+      if (ok) qf[ks] = q_src[2 * ks];
+    }
+    const int32_t qp = ok ? p.q_pos[node] : INT32_MIN;
+    int32_t q_min = ok ? qp : INT32_MAX;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) q_min = min(q_min, __shfl_xor(q_min, o, 64));
+
+    float ref = -INFINITY, l_run = 0.f;
+    floatx16_t o_acc[NCB], s[2];
+    u32x4_t pb[2][TERMS][2];               // P of the current sub-tile and the one before, in bf16 pairs per
+                                           // term (keys 0..15, 16..31)
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) pb[1][k][0] = pb[1][k][1] = u32x4_t{0, 0, 0, 0};
+    bool pending = false;                  // O^T of the sub-tile before has not been added yet
+#pragma unroll
+    for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o_acc[cb][i] = 0.f;
+
+    // (LDS addresses as numbers: `sub` is one of the wavefront's, uniform)
+    auto lds = [](const char* sub) { return (uint32_t)(size_t)(CP_LDS_AS const char*)sub; };
+    auto k_frag = [&](const char* sub, int ks) __attribute__((always_inline)) {
+      return __builtin_bit_cast(uint4, *(CP_LDS_AS const u32x4_t*)(size_t)((lds(sub) + koff) ^ (ks * 32)));
+    };
+    auto v_frag = [&](const char* sub, int f) __attribute__((always_inline)) -> uint4 {   // f = cb * 2 + kb
+      u32x4_t v;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const u32x2_t z = __builtin_bit_cast(
+            u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((CP_LDS_AS shortx4_t*)(size_t)(
+                         (((lds(sub) + M::V_OFF + voff) ^ ((f >> 1) * 64)) + ((f & 1) * 16 + x * 8) * T::ROW))));
+        v[2 * x] = z[0];
+        v[2 * x + 1] = z[1];
+      }
+      return __builtin_bit_cast(uint4, v);
+    };
+    // O^T of a sub-tile with nothing in between. ODD: V holds what is not finite, which reaches the rows
+    // that see it, and no other.
+    auto value_product = [&](auto parc, auto oddc, const char* sub) __attribute__((always_inline)) {
+      constexpr int par = decltype(parc)::value;
+      constexpr bool odd_v = decltype(oddc)::value != 0;
+#pragma unroll
+      for (int cb = 0; cb < NCB; ++cb) {
+        u32x4_t v[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) v[kb] = __builtin_bit_cast(u32x4_t, v_frag(sub, cb * 2 + kb));
+        if constexpr (odd_v) {
+          const u32x4_t t[2] = {pb[par][0][0], pb[par][0][1]};
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              floatx16_t sign;   // how many visible infinities of this sign (a NaN counts for both)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) sign[i] = 0.f;
+#pragma unroll
+              for (int kb = 0; kb < 2; ++kb) {
+                u32x4_t a, seen;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                  a[x] = not_finite(v[kb][x], m == 1);
+                  seen[x] = ((t[kb][x] & 0xffffu) != 0 ? 0x3f80u : 0) | ((t[kb][x] >> 16) != 0 ? 0x3f800000u : 0);
+                }
+                sign = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, seen), sign);
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o_acc[cb][i] += sign[i] > 0.f ? (m == 0 ? INFINITY : -INFINITY) : 0.f;
+            }
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+              for (int x = 0; x < 4; ++x) v[kb][x] = only_finite(v[kb][x]);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int k = 0; k < TERMS; ++k)
+            o_acc[cb] = mfma32(__builtin_bit_cast(bf16x8_t, v[kb]), __builtin_bit_cast(bf16x8_t, pb[par][k][kb]),
+                               o_acc[cb]);
+      }
+    };
+
+    // One step: softmax of sub-tile st (scores s[PAR], positions at `pos`, values at v_here), products S^T
+    // of the next one (K rows at k_next) and O^T of the one before (V rows at v_prev). Returns whether
+    // the sub-tile's V holds what is not finite and is hidden from a row.
+    auto step = [&](auto parc, int st, const int32_t* pos, const char* v_here, const char* k_next,
+                    const char* v_prev) __attribute__((always_inline)) -> bool {
+      constexpr int PAR = decltype(parc)::value;
+      // K fragments 0 .. NKS-1 of the next sub-tile, then V^T fragments of the one before: AHEAD of them
+      // are on their way
+      constexpr int FRAGS = NKS + NVF, AHEAD = 4;
+      uint4 fr[AHEAD];
+      auto request = [&](int g) __attribute__((always_inline)) {
+        if (g < NKS) fr[g % AHEAD] = k_frag(k_next, g);
+        else if (g < FRAGS) fr[g % AHEAD] = v_frag(v_prev, (g - NKS) % NCB * 2 + (g - NKS) / NCB);
+      };
+#pragma unroll
+      for (int g = 0; g < AHEAD; ++g) request(g);
+      const bool own = st >= n_cached;
+      const int cnt = own ? sq.n - (st - n_cached) * SUB : sq.used - st * SUB;   // keys, if not SUB
+      bool masked = own || cnt < SUB;
+      if (!masked) masked = __builtin_amdgcn_ballot_w64(pos[rl] > q_min) != 0;
+      uint32_t odd_here = 0;
+      if (masked) {
+        const uint32_t there = st >= n_subs ? 0 : cnt >= SUB ? ~0u : (1u << cnt) - 1;
+        uint32_t see = there;
+        if (own) {
+          const int word = (st - n_cached) >> 1;
+          see = 0;
+          if (ok && word < p.words && there != 0)
+            see = (uint32_t)(p.mask[(int64_t)node * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
+        }
+        see >>= hf * 4;   // (bit a * 8 + i: score 4 a + i)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const int4 x = *(const int4*)(pos + a * 8 + hf * 4);
+          const int32_t kp[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int vis = (int)((see & (1u << (a * 8 + i))) != 0) & ((int)own | (int)(kp[i] <= qp));
+            s[PAR][4 * a + i] = vis != 0 ? s[PAR][4 * a + i] : -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < SUB * T::ROW / 1024; ++i) {
+          const uint4 x = *(const uint4*)(v_here + M::V_OFF + i * 1024 + lane * 16);
+          odd_here |= any_not_finite(x.x) | any_not_finite(x.y) | any_not_finite(x.z) | any_not_finite(x.w);
+        }
+        odd_here = __builtin_amdgcn_ballot_w64(odd_here != 0) != 0;
+      }
+      float mx = fmaxf(fmaxf(s[PAR][0], s[PAR][1]), s[PAR][2]);
+#pragma unroll
+      for (int i = 3; i < 15; i += 2) mx = fmaxf(fmaxf(mx, s[PAR][i]), s[PAR][i + 1]);
+      mx = halves_max(fmaxf(mx, s[PAR][15])) * p.scale_log2;
+      const bool raise = mx > ref + kSlack;
+      const bool any_raise = __builtin_amdgcn_ballot_w64(raise) != 0;
+      float alpha = 1.f;
+      if (any_raise) {
+        if (raise) {
+          alpha = __builtin_amdgcn_exp2f(ref - mx);
+          ref = mx;
+        }
+        l_run *= alpha;
+      }
+      const float use = ref == -INFINITY ? 0.f : ref;
+
+      // Softmax arithmetic in units, two MFMA slots or so apart: argument of score w, exponential of the
+      // one before, sum and rounding of the one before that.
+      constexpr int UNITS = 18, SLOTS = NKS + NVF * TERMS;
+      float e[16], sum[2] = {0.f, 0.f};
+      auto unit = [&](int w) __attribute__((always_inline)) {
+        if (w >= 2) {
+          const int i = w - 2;
+          sum[i & 1] += e[i];
+          if ((i & 1) == 1)
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) {
+              const uint32_t x = pack_bf16(e[i - 1], e[i]);
+              pb[PAR][k][i >> 3][(i & 7) >> 1] = x;
+              if (k + 1 < TERMS) {   // what the term leaves over (exact)
+                e[i - 1] -= __builtin_bit_cast(float, x << 16);
+                e[i] -= __builtin_bit_cast(float, x & 0xffff0000u);
+              }
+            }
+        }
+        if (w >= 1 && w < 17) e[w - 1] = __builtin_amdgcn_exp2f(e[w - 1]);
+        if (w < 16) e[w] = fmaf(s[PAR][w], p.scale_log2, -use);
+      };
+      auto units = [&](int slot) __attribute__((always_inline)) {
+#pragma unroll
+        for (int w = slot * UNITS / SLOTS; w < (slot + 1) * UNITS / SLOTS; ++w) unit(w);
+        __builtin_amdgcn_sched_barrier(0);
+      };
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[PAR ^ 1][i] = 0.f;
+#pragma unroll
+      for (int g = 0; g < FRAGS; ++g) {
+        const bf16x8_t a = __builtin_bit_cast(bf16x8_t, fr[g % AHEAD]);
+        if (g < NKS) {
+          s[PAR ^ 1] = mfma32(a, __builtin_bit_cast(bf16x8_t, qf[g < NKS ? g : 0]), s[PAR ^ 1]);
+          request(g + AHEAD);
+          units(g);
+        } else {
+          // (neighbouring fragments belong to different blocks of O)
+          const int f = g - NKS, cb = f % NCB, kb = f / NCB;
+#pragma unroll
+          for (int k = 0; k < TERMS; ++k) {
+            o_acc[cb] = mfma32(a, __builtin_bit_cast(bf16x8_t, pb[PAR ^ 1][k][kb]), o_acc[cb]);
+            if (k == TERMS - 1) request(g + AHEAD);
+            units(NKS + f * TERMS + k);
+          }
+        }
+      }
+      l_run += sum[0] + sum[1];
+      // (all of this belongs in front of the branch below: the optimiser would sink it behind it)
+      pin(s[PAR ^ 1]);
+      pin(l_run);
+#pragma unroll
+      for (int k = 0; k < TERMS; ++k)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) pin(pb[PAR][k][kb]);
+#pragma unroll
+      for (int cb = 0; cb < NCB; ++cb) pin(o_acc[cb]);
+      if (any_raise) {
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o_acc[cb][i] *= alpha;
+      }
+      return odd_here != 0;
+    };
+    auto run_step = [&](auto parc, int st, const int32_t* pos, const char* v_here, const char* k_next,
+                        const char* v_prev) __attribute__((always_inline)) {
+      // (no product is pending: P times zeros)
+      const bool odd = step(parc, st, pos, v_here, k_next, pending ? v_prev : smem + M::ZERO_OFF - M::V_OFF);
+      if (__builtin_expect(odd, 0)) value_product(parc, IntC<1>{}, v_here);
+      pending = !odd;
+    };
+
+    if (n_subs > 0) {
+      constexpr int HALF = SUB * T::ROW;   // bytes from a tile's first sub-tile to its second
+      char *prev = smem, *cur = smem + M::BYTES, *next = smem + 2 * M::BYTES;
+      lds_barrier();   // the piece before has been read
+      put(cur);
+      if (pc.t0 + 1 < pc.t1) fetch(pc.t0 + 1);
+      lds_barrier();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks)
+        s[0] = mfma32(__builtin_bit_cast(bf16x8_t, k_frag(cur, ks)), __builtin_bit_cast(bf16x8_t, qf[ks]), s[0]);
+      for (int t = pc.t0; t < pc.t1; ++t) {
+        const int32_t* const pos = (const int32_t*)(cur + M::POS_OFF);
+        run_step(IntC<0>{}, 2 * t, pos, cur, cur + HALF, prev + HALF);
+        if (t + 1 < pc.t1) {
+          put(next);
+          if (t + 2 < pc.t1) fetch(t + 2);
+        }
+        lds_barrier();
+        // (a second sub-tile that is not there holds copies of the last key, none of which counts)
+        run_step(IntC<1>{}, 2 * t + 1, pos + SUB, cur + HALF, next, cur);
+        char* const x = prev;
+        prev = cur;
+        cur = next;
+        next = x;
+      }
+      if (pending) value_product(IntC<1>{}, IntC<0>{}, prev + HALF);
+    }
+    l_run += xor32(l_run);
+
+    // ---- the span's result, or this share's part of it ----
+    if (ok) {
+      float inv = 1.f;
+      TO* out = nullptr;
+      float* part = nullptr;
+      if (pc.whole) {
+        const int64_t at = (int64_t)node * p.n_q_heads + head;
+        inv = l_run > 0.f ? 1.f / l_run : l_run == 0.f ? 0.f : l_run;   // (a NaN stays one)
+        out = (TO*)p.out + at * D;
+        if (hf == 0) p.lse[at] = l_run == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l_run)) * kLn2;
+      } else {
+        const int64_t at = (int64_t)pc.slot * MANY_ROWS + wave * 32 + rl;
+        part = p.part_o + at * D;
+        if (hf == 0) {
+          p.part_ml[at * 2] = ref;
+          p.part_ml[at * 2 + 1] = l_run;
+        }
+      }
+#pragma unroll
+      for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+          const floatx4_t x = {o_acc[cb][4 * a], o_acc[cb][4 * a + 1], o_acc[cb][4 * a + 2], o_acc[cb][4 * a + 3]};
+          const int ch = cb * 32 + a * 8 + hf * 4;
+          if (pc.whole) store4<TO>(out + ch, x * inv);
+          else *(floatx4_t*)(part + ch) = x;
+        }
+    }
+    u += pc.t1 - pc.t0;
+  }
+}
+
 // Joins the parts of the spans that fell into several shares, a wavefront per row: lane l knows the
 // maximum and sum of part l, and the rows of eight parts are in flight at a time.
 template <int D, int RM, int SPT, typename TO>
@@ -803,14 +1221,12 @@ struct TreePlan {
   int rm, spt, n_wg, log2_wg, min_share;
   size_t o_bytes, ml_bytes;
 };
-constexpr int kManyWaves = 8;
-
 TreePlan tree_plan(const cp_shape& s) {
   TreePlan pl = {};
   const int64_t group = s.n_q_heads / s.n_kv_heads;
   const int64_t rows = s.total_q * group / s.batch;   // of a sequence, on average
   pl.form = s.dtype == CP_FP32 || rows <= 32 ? kFew32 : rows <= 128 ? kFew64 : kMany;
-  pl.rm = pl.form == kFew32 ? 32 : pl.form == kFew64 ? 64 : 32 * kManyWaves;
+  pl.rm = pl.form == kFew32 ? 32 : pl.form == kFew64 ? 64 : MANY_ROWS;
   pl.spt = pl.form == kMany ? 2 : 4;
   pl.min_share = 1;
   // no more workgroups than there can be tiles
@@ -843,11 +1259,26 @@ int launch_form(const TreeParams& p, hipStream_t st) {
 }
 
 template <int D, int TERMS, typename TO>
+int launch_many(const TreeParams& p, hipStream_t st) {
+  static_assert(ManyTile<D>::SMEM <= 160 * 1024, "LDS of a CU");
+  auto kernel = tree_many_kernel<D, TERMS, TO>;
+  if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize,
+                          ManyTile<D>::SMEM) != hipSuccess)
+    return CP_ERR_LAUNCH;
+  hipLaunchKernelGGL(kernel, dim3(p.n_wg), dim3(MANY_WAVES * 64), ManyTile<D>::SMEM, st, p);
+  if (check_launch() != CP_OK) return CP_ERR_LAUNCH;
+  const int64_t rows = p.total_q * p.n_q_heads;
+  hipLaunchKernelGGL((tree_join_kernel<D, MANY_ROWS, 2, TO>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st,
+                     p);
+  return check_launch();
+}
+
+template <int D, int TERMS, typename TO>
 int launch_bf16(const TreeParams& p, TreeForm form, hipStream_t st) {
   switch (form) {
     case kFew32: return launch_form<bf16_t, D, true, 1, 4, TERMS, TO>(p, st);
     case kFew64: return launch_form<bf16_t, D, true, 2, 4, TERMS, TO>(p, st);
-    default: return launch_form<bf16_t, D, false, 1, kManyWaves, TERMS, TO>(p, st);
+    default: return launch_many<D, TERMS, TO>(p, st);
   }
 }
 
