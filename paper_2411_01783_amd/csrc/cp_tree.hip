@@ -53,7 +53,6 @@ struct TreeParams {
   int64_t total_q, total_kv;
   int32_t batch, words, n_q_heads, n_kv_heads, group;
   int32_t n_wg, log2_wg;   // workgroups among which the line is dealt out, a power of two
-  int32_t min_share;
   float scale_log2;
 };
 
@@ -120,7 +119,6 @@ struct TreeLine {
     }
     const int64_t all = head_tiles * p.n_kv_heads;
     share = (all + p.n_wg - 1) >> p.log2_wg;
-    if (share < p.min_share) share = p.min_share;
   }
   // The sequence of tile u of a KV head (-1: behind the last), and the tile where it begins.
   __device__ __forceinline__ int find(int64_t u, int64_t* begin, TreeSeq* sq) {
@@ -235,6 +233,13 @@ __device__ __forceinline__ void store4<bf16_t>(bf16_t* dst, floatx4_t x) {
   *(bf16x4_t*)dst = y;
 }
 
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  bf16x2_t t;
+  t[0] = static_cast<bf16_t>(a);
+  t[1] = static_cast<bf16_t>(b);
+  return __builtin_bit_cast(uint32_t, t);
+}
+
 // bf16 pairs: 1.0 where the element is not finite and not of sign `minus` (a NaN counts for both),
 // else 0; and the pair with what is not finite replaced by zero.
 __device__ __forceinline__ uint32_t not_finite(uint32_t x, bool minus) {
@@ -256,28 +261,23 @@ __device__ __forceinline__ uint32_t any_not_finite(uint32_t x) {   // 1 or 0, wi
   return (uint32_t)((x & 0x7f80u) == 0x7f80u) | (uint32_t)((x & 0x7f800000u) == 0x7f800000u);
 }
 
-// KS: the wavefronts of a workgroup hold the same 32 C rows and take turns at the sub-tiles (few
-// rows: the keys are what there is to share out). Otherwise every wavefront holds 32 C rows of its
-// own and all read every sub-tile of a tile.
-template <bool KS, int C, int NW>
-struct Form {
-  static constexpr int RW = 32 * C;                    // rows of a wavefront
-  static constexpr int RM = KS ? RW : RW * NW;         // rows of a row block
-  static constexpr int SPT = KS ? NW : 2;              // sub-tiles of a tile
-};
-template <typename TI, int D, bool KS, int C, int NW>
-constexpr int tree_smem() {
-  using F = Form<KS, C, NW>;
-  const int tiles = F::SPT * SubTile<TI, D>::BYTES;
-  const int join = KS ? NW * (F::RW * (D + 4) + 2 * F::RW) * 4 : 0;
+// Few rows: the four wavefronts of a workgroup hold the same 32 rows and take turns at the sub-tiles (the keys
+// are what there is to share out), each with a buffer of its own; a tile is a sub-tile for each of them.
+constexpr int FEW_WAVES = 4, FEW_ROWS = 32;
+template <typename TI, int D>
+constexpr int few_smem() {
+  const int tiles = FEW_WAVES * SubTile<TI, D>::BYTES;
+  const int join = FEW_WAVES * FEW_ROWS * (D + 4 + 2) * 4;
   return tiles > join ? tiles : join;
 }
 
+// Bound by latencies: the chain {sequence boundaries} -> K, V, Q -> products -> join in LDS -> parts, and the
+// second launch; 8 nodes of 16 heads over 430 keys take 9 us here and 4 in the join, 32 sequences of 4096 keys at
+// 32 rows each 29.7 us (67 MB, 2.3 TB/s).
 // TI: K, V and Q. TO: O. P goes into the second product as TERMS bf16 terms (bf16 inputs): one
 // where O is rounded to bf16 itself, three (24 bits) where it stays fp32.
-template <typename TI, int D, bool KS, int C, int NW, int TERMS, typename TO>
-__global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) {
-  using F = Form<KS, C, NW>;
+template <typename TI, int D, int TERMS, typename TO>
+__global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void tree_few_kernel(const TreeParams p) {
   using T = SubTile<TI, D>;
   constexpr bool F32 = sizeof(TI) == 4;
   constexpr int NKS = T::ROW / 32, NCB = D / 32;
@@ -285,7 +285,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rl = lane & 31, hf = lane >> 5;   // row (N side) or key / channel (M side), half
-  TreeLine<F::RM, F::SPT> line(p);
+  TreeLine<FEW_ROWS, FEW_WAVES> line(p);
   int64_t u = blockIdx.x * line.share;
   const int64_t u_end = min(line.head_tiles * p.n_kv_heads, u + line.share);
   const int64_t tok_q = (int64_t)p.n_q_heads * D, tok_kv = (int64_t)p.n_kv_heads * D;
@@ -297,72 +297,65 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
     const int kvh = pc.kvh, t0 = pc.t0, t1 = pc.t1, n_cached = pc.n_cached, n_subs = pc.n_subs;
     const int n_rows = sq.n * p.group;
 
+    // Requests for sub-tile `st`: rows behind its last one repeat that one (and are masked by their index).
+    char* const buf = smem + wave * T::BYTES;
+    auto request = [&](int st) __attribute__((always_inline)) {
+      const bool own = st >= n_cached;
+      const int first = (own ? st - n_cached : st) * SUB;
+      const int last = min(SUB, (own ? sq.n : sq.used) - first) - 1;
+      const int64_t base = (int64_t)(own ? sq.q0 : sq.k0) + first;
+      const TI *kt = (const TI*)p.k, *vt = (const TI*)p.v;
+      if (own) {
+        kt = (const TI*)p.k_new;
+        vt = (const TI*)p.v_new;
+      }
+      kt += base * tok_kv + kvh * D;
+      vt += base * tok_kv + kvh * D;
+      constexpr int RPI = 64 / T::CH;          // rows of a request
+#pragma unroll
+      for (int i = 0; i < SUB / RPI; ++i) {
+        const int r = i * RPI + lane / T::CH, slot = lane % T::CH;
+        const int64_t off = min(r, last) * tok_kv;
+        to_lds16((const uint4*)(kt + off) + (slot ^ T::k_perm(r)), buf + i * 1024);
+        to_lds16((const uint4*)(vt + off) + (slot ^ T::v_perm(r)), buf + T::V_OFF + i * 1024);
+      }
+      if (!own)
+        __builtin_amdgcn_global_load_lds((const CP_GLB_AS void*)(p.kv_pos + base + min(rl, last)),
+                                         (CP_LDS_AS void*)(buf + T::POS_OFF), 4, 0, 0);
+    };
+    lds_barrier();   // what the piece before joined has been read
+    if (t0 * FEW_WAVES + wave < n_subs) request(t0 * FEW_WAVES + wave);
+
     // ---- the wavefront's rows ----
-    int row[C];            // within (sequence, KV head)
-    int node[C];           // of all nodes; -1: a row behind the last one
-    int32_t qp[C];
-    uint4 qf[C][NKS];      // lane (rl, hf): 16-byte chunk 2 ks + hf of row rl
-    int32_t q_min = INT32_MAX, q_max = INT32_MIN;
+    const int row = pc.span * FEW_ROWS + rl;   // within (sequence, KV head)
+    const bool ok = row < n_rows;
+    const int nd = ok ? (uint32_t)row / (uint32_t)p.group : 0;
+    const int node = sq.q0 + nd;
+    const int head = kvh * p.group + (ok ? row - nd * p.group : 0);
+    const uint4* const q_src = (const uint4*)((const TI*)p.q + node * tok_q + head * D) + hf;
+    uint4 qf[NKS];      // lane (rl, hf): 16-byte chunk 2 ks + hf of row rl
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      row[c] = pc.span * F::RM + (KS ? 0 : wave * F::RW) + c * 32 + rl;
-      const bool ok = row[c] < n_rows;
-      const int nd = ok ? (uint32_t)row[c] / (uint32_t)p.group : 0;
-      node[c] = ok ? sq.q0 + nd : -1;
-      const int head = kvh * p.group + (ok ? row[c] - nd * p.group : 0);
-      const uint4* src = (const uint4*)((const TI*)p.q + (ok ? node[c] : 0) * tok_q + head * D) + hf;
-#pragma unroll
-      for (int ks = 0; ks < NKS; ++ks) {
-        qf[c][ks] = make_uint4(0, 0, 0, 0);
-        if (ok) qf[c][ks] = src[2 * ks];
-      }
-      qp[c] = ok ? p.q_pos[node[c]] : INT32_MIN;
-      if (ok) {
-        q_min = min(q_min, qp[c]);
-        q_max = max(q_max, qp[c]);
-      }
+    for (int ks = 0; ks < NKS; ++ks) {
+      qf[ks] = make_uint4(0, 0, 0, 0);
+      if (ok) qf[ks] = q_src[2 * ks];
     }
+    const int32_t qp = ok ? p.q_pos[node] : INT32_MIN;
+    int32_t q_min = ok ? qp : INT32_MAX, q_max = qp;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
       q_min = min(q_min, __shfl_xor(q_min, o, 64));
       q_max = max(q_max, __shfl_xor(q_max, o, 64));
     }
 
-    float m_run[C], l_run[C];
-    floatx16_t o_acc[C][NCB];
+    float m_run = -INFINITY, l_run = 0.f;
+    floatx16_t o_acc[NCB];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      m_run[c] = -INFINITY;
-      l_run[c] = 0.f;
+    for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-      for (int cb = 0; cb < NCB; ++cb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o_acc[c][cb][i] = 0.f;
-    }
-
-    // Requests for sub-tile `st` into LDS at `dst`: rows behind its last one repeat that one (and are
-    // masked by their index). `w` of `nw` wavefronts share the requests out.
-    auto request = [&](int st, char* dst, int w, int nw) {
-      const bool own = st >= n_cached;
-      const int first = (own ? st - n_cached : st) * SUB;
-      const int last = min(SUB, (own ? sq.n : sq.used) - first) - 1;
-      const int64_t base = (int64_t)(own ? sq.q0 : sq.k0) + first;
-      const TI* kt = (const TI*)(own ? p.k_new : p.k) + base * tok_kv + kvh * D;
-      const TI* vt = (const TI*)(own ? p.v_new : p.v) + base * tok_kv + kvh * D;
-      constexpr int RPI = 64 / T::CH;          // rows of a request
-      for (int i = w; i < SUB / RPI; i += nw) {
-        const int r = i * RPI + lane / T::CH, slot = lane % T::CH;
-        const int64_t off = (int64_t)min(r, last) * tok_kv;
-        to_lds16((const uint4*)(kt + off) + (slot ^ T::k_perm(r)), dst + i * 1024);
-        to_lds16((const uint4*)(vt + off) + (slot ^ T::v_perm(r)), dst + T::V_OFF + i * 1024);
-      }
-      if (!own && w == 0)
-        __builtin_amdgcn_global_load_lds((const CP_GLB_AS void*)(p.kv_pos + base + min(rl, last)),
-                                         (CP_LDS_AS void*)(dst + T::POS_OFF), 4, 0, 0);
-    };
+      for (int i = 0; i < 16; ++i) o_acc[cb][i] = 0.f;
 
     // S, P and O of one sub-tile that lies in LDS at `buf`.
-    auto compute = [&](int st, const char* buf) {
+    auto compute = [&](int st) __attribute__((always_inline)) {
       const bool own = st >= n_cached;
       const int first = (own ? st - n_cached : st) * SUB;
       const int cnt = min(SUB, (own ? sq.n : sq.used) - first);
@@ -372,53 +365,41 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
         if (__builtin_amdgcn_ballot_w64(kp <= q_max) == 0) return;   // none of the rows sees any
         masked = masked || __builtin_amdgcn_ballot_w64(kp > q_min) != 0;
       }
-      floatx16_t s[C];
+      floatx16_t s;
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[c][i] = 0.f;
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < NKS; ++ks) {
         const uint4 a = *(const uint4*)(buf + rl * T::ROW + (((2 * ks + hf) ^ T::k_perm(rl)) << 4));
+        if constexpr (F32) {
+          const floatx4_t af = __builtin_bit_cast(floatx4_t, a);
+          const floatx4_t qv = __builtin_bit_cast(floatx4_t, qf[ks]);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          if constexpr (F32) {
-            const floatx4_t af = __builtin_bit_cast(floatx4_t, a);
-            const floatx4_t qv = __builtin_bit_cast(floatx4_t, qf[c][ks]);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) s[c] = mfma32(af[x], qv[x], s[c]);
-          } else {
-            s[c] = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, qf[c][ks]),
-                          s[c]);
-          }
+          for (int x = 0; x < 4; ++x) s = mfma32(af[x], qv[x], s);
+        } else {
+          s = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, qf[ks]), s);
         }
       }
       // score i of lane (rl, hf): key (i / 4) * 8 + hf * 4 + i % 4
       bool odd_v = false;   // V holds what is not finite, which rows that do not see it must not meet
       if (masked) {
         const uint32_t there = cnt == SUB ? ~0u : (1u << cnt) - 1;
-        int32_t kp[16];
-        if (!own) {
-#pragma unroll
-          for (int a = 0; a < 4; ++a) {
-            const int4 x = *(const int4*)(buf + T::POS_OFF + (a * 8 + hf * 4) * 4);
-            kp[4 * a] = x.x; kp[4 * a + 1] = x.y; kp[4 * a + 2] = x.z; kp[4 * a + 3] = x.w;
-          }
+        uint32_t see = there;
+        if (own) {
+          const int word = (st - n_cached) >> 1;
+          see = 0;
+          if (ok && word < p.words)
+            see = (uint32_t)(p.mask[(int64_t)node * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
         }
+        see >>= hf * 4;   // (bit a * 8 + i: score 4 a + i)
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-          uint32_t see = there;
-          if (own) {
-            const int word = (st - n_cached) >> 1;
-            see = 0;
-            if (node[c] >= 0 && word < p.words)
-              see = (uint32_t)(p.mask[(int64_t)node[c] * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
-          }
+        for (int a = 0; a < 4; ++a) {
+          const int4 x = *(const int4*)(buf + T::POS_OFF + (a * 8 + hf * 4) * 4);
+          const int32_t kp[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const bool vis = ((see >> ((i >> 2) * 8 + hf * 4 + (i & 3))) & 1) != 0 &&
-                             (own || kp[i] <= qp[c]);
-            s[c][i] = vis ? s[c][i] : -INFINITY;
+          for (int i = 0; i < 4; ++i) {
+            const int vis = (int)((see & (1u << (a * 8 + i))) != 0) & ((int)own | (int)(kp[i] <= qp));
+            s[4 * a + i] = vis != 0 ? s[4 * a + i] : -INFINITY;
           }
         }
 #pragma unroll
@@ -433,53 +414,44 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
         }
         odd_v = __builtin_amdgcn_ballot_w64(odd_v) != 0;
       }
-      u32x4_t pb[C][TERMS][2];   // P^T of keys 0..15 and 16..31, per term
-      float pf[C][F32 ? 16 : 1];
+      u32x4_t pb[TERMS][2];   // P^T of keys 0..15 and 16..31, per term
+      float e[16];
+      float mx = s[0];
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float mx = s[c][0];
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+      mx = fmaxf(mx, xor32(mx));
+      const float m_new = fmaxf(m_run, mx * p.scale_log2);
+      const float m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+      m_run = m_new;
+      float sum = 0.f;
 #pragma unroll
-        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[c][i]);
-        mx = fmaxf(mx, xor32(mx));
-        const float m_new = fmaxf(m_run[c], mx * p.scale_log2);
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = __builtin_amdgcn_exp2f(m_run[c] - m_use);
-        m_run[c] = m_new;
-        float sum = 0.f;
+      for (int i = 0; i < 16; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -m_use));
+        sum += e[i];
+        if (!F32 && (i & 1) == 1)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float e = __builtin_amdgcn_exp2f(fmaf(s[c][i], p.scale_log2, -m_use));
-          sum += e;
-          if constexpr (F32) {
-            pf[c][i] = e;
-          } else {
-#pragma unroll
-            for (int t = 0; t < TERMS; ++t) {
-              const bf16_t x = static_cast<bf16_t>(e);
-              const uint32_t bits = __builtin_bit_cast(uint16_t, x);
-              if ((i & 1) == 0) pb[c][t][i >> 3][(i & 7) >> 1] = bits;
-              else pb[c][t][i >> 3][(i & 7) >> 1] |= bits << 16;
-              e -= static_cast<float>(x);
-            }
+          for (int t = 0; t < TERMS; ++t) {
+            const uint32_t x = pack_bf16(e[i - 1], e[i]);
+            pb[t][i >> 3][(i & 7) >> 1] = x;
+            e[i - 1] -= __builtin_bit_cast(float, x << 16);   // what the term leaves over (exact)
+            e[i] -= __builtin_bit_cast(float, x & 0xffff0000u);
           }
-        }
-        l_run[c] = fmaf(l_run[c], alpha, sum);
-        if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
+      }
+      l_run = fmaf(l_run, alpha, sum);
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.f) != 0) {
 #pragma unroll
-          for (int cb = 0; cb < NCB; ++cb)
+        for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o_acc[c][cb][i] *= alpha;
-        }
+          for (int i = 0; i < 16; ++i) o_acc[cb][i] *= alpha;
       }
       if constexpr (F32) {
         // O^T += V^T P^T, a key pair a step: k slot hf of step i is the key of score i
 #pragma unroll
         for (int cb = 0; cb < NCB; ++cb) {
-          floatx16_t plus[C], minus[C];   // how many visible infinities of either sign (a NaN: both)
+          floatx16_t plus, minus;   // how many visible infinities of either sign (a NaN: both)
 #pragma unroll
-          for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) plus[c][i] = minus[c][i] = 0.f;
+          for (int i = 0; i < 16; ++i) plus[i] = minus[i] = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int r = (i >> 2) * 8 + hf * 4 + (i & 3);
@@ -487,23 +459,17 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
             if (odd_v) {
               const bool fin = fabsf(v) < INFINITY;
               const float up = fin || v == -INFINITY ? 0.f : 1.f, dn = fin || v == INFINITY ? 0.f : 1.f;
-#pragma unroll
-              for (int c = 0; c < C; ++c) {
-                const float seen = pf[c][i] != 0.f ? 1.f : 0.f;
-                plus[c] = mfma32(up, seen, plus[c]);
-                minus[c] = mfma32(dn, seen, minus[c]);
-              }
+              const float seen = e[i] != 0.f ? 1.f : 0.f;
+              plus = mfma32(up, seen, plus);
+              minus = mfma32(dn, seen, minus);
               v = fin ? v : 0.f;
             }
-#pragma unroll
-            for (int c = 0; c < C; ++c) o_acc[c][cb] = mfma32(v, pf[c][i], o_acc[c][cb]);
+            o_acc[cb] = mfma32(v, e[i], o_acc[cb]);
           }
           if (odd_v) {
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                o_acc[c][cb][i] += (plus[c][i] > 0.f ? INFINITY : 0.f) + (minus[c][i] > 0.f ? -INFINITY : 0.f);
+            for (int i = 0; i < 16; ++i)
+              o_acc[cb][i] += (plus[i] > 0.f ? INFINITY : 0.f) + (minus[i] > 0.f ? -INFINITY : 0.f);
           }
         }
       } else {
@@ -525,30 +491,26 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
               v[kb][2 * x + 1] = z[1];
             }
           if (__builtin_expect(odd_v, 0)) {
+            floatx16_t sign[2];   // how many visible infinities of either sign (a NaN: both)
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-              floatx16_t sign[2];   // how many visible infinities of either sign (a NaN: both)
+            for (int m = 0; m < 2; ++m) {
 #pragma unroll
-              for (int m = 0; m < 2; ++m) {
+              for (int i = 0; i < 16; ++i) sign[m][i] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sign[m][i] = 0.f;
+              for (int kb = 0; kb < 2; ++kb) {
+                u32x4_t a, seen;
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                  u32x4_t a, seen;
-#pragma unroll
-                  for (int x = 0; x < 4; ++x) {
-                    a[x] = not_finite(v[kb][x], m == 1);
-                    seen[x] = ((pb[c][0][kb][x] & 0xffffu) != 0 ? 0x3f80u : 0) |
-                              ((pb[c][0][kb][x] >> 16) != 0 ? 0x3f800000u : 0);
-                  }
-                  sign[m] = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, seen),
-                                   sign[m]);
+                for (int x = 0; x < 4; ++x) {
+                  a[x] = not_finite(v[kb][x], m == 1);
+                  seen[x] = ((pb[0][kb][x] & 0xffffu) != 0 ? 0x3f80u : 0) |
+                            ((pb[0][kb][x] >> 16) != 0 ? 0x3f800000u : 0);
                 }
+                sign[m] = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, seen), sign[m]);
               }
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                o_acc[c][cb][i] += (sign[0][i] > 0.f ? INFINITY : 0.f) + (sign[1][i] > 0.f ? -INFINITY : 0.f);
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              o_acc[cb][i] += (sign[0][i] > 0.f ? INFINITY : 0.f) + (sign[1][i] > 0.f ? -INFINITY : 0.f);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -557,36 +519,22 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int c = 0; c < C; ++c)
-#pragma unroll
-              for (int t = 0; t < TERMS; ++t)
-                o_acc[c][cb] = mfma32(__builtin_bit_cast(bf16x8_t, v[kb]),
-                                      __builtin_bit_cast(bf16x8_t, pb[c][t][kb]), o_acc[c][cb]);
+            for (int t = 0; t < TERMS; ++t)
+              o_acc[cb] = mfma32(__builtin_bit_cast(bf16x8_t, v[kb]), __builtin_bit_cast(bf16x8_t, pb[t][kb]),
+                                 o_acc[cb]);
         }
       }
     };
 
-    for (int t = t0; t < t1; ++t) {
-      __syncthreads();   // the tile before has been read
-      if (KS) {
-        const int st = t * F::SPT + wave;
-        if (st < n_subs) request(st, smem + wave * T::BYTES, 0, 1);
-      } else {
-        for (int x = 0; x < F::SPT; ++x)
-          if (t * F::SPT + x < n_subs) request(t * F::SPT + x, smem + x * T::BYTES, wave, NW);
-      }
+    for (int t = t0; t < t1; ++t) {   // (a wavefront waits for its own sub-tiles alone)
+      const int st = t * FEW_WAVES + wave;
+      if (st >= n_subs) break;
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (KS) {
-        const int st = t * F::SPT + wave;
-        if (st < n_subs) compute(st, smem + wave * T::BYTES);
-      } else {
-        for (int x = 0; x < F::SPT; ++x)
-          if (t * F::SPT + x < n_subs) compute(t * F::SPT + x, smem + x * T::BYTES);
-      }
+      compute(st);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (t + 1 < t1 && st + FEW_WAVES < n_subs) request(st + FEW_WAVES);
     }
-#pragma unroll
-    for (int c = 0; c < C; ++c) l_run[c] += xor32(l_run[c]);
+    l_run += xor32(l_run);
 
     // ---- the span's result, or this share's part of it ----
     auto write = [&](int r, int in_block, float m, float l, int ch, floatx4_t o4) {
@@ -598,7 +546,7 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
         store4<TO>((TO*)p.out + at * D + ch, o4 * inv);
         if (ch == 0) p.lse[at] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
       } else {
-        const int64_t at = (int64_t)pc.slot * F::RM + in_block;
+        const int64_t at = (int64_t)pc.slot * FEW_ROWS + in_block;
         *(floatx4_t*)(p.part_o + at * D + ch) = o4;
         if (ch == 0) {
           p.part_ml[at * 2] = m;
@@ -606,56 +554,46 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
         }
       }
     };
-    if constexpr (KS) {
-      // the wavefronts' disjoint subsets of the keys are joined in LDS
-      constexpr int OS = D + 4;                      // floats of a row
-      constexpr int WS = F::RW * OS + 2 * F::RW;     // of a wavefront
-      float* const cb0 = (float*)smem;
-      __syncthreads();
+    // the wavefronts' disjoint subsets of the keys are joined in LDS
+    constexpr int OS = D + 4;                      // floats of a row
+    constexpr int WS = FEW_ROWS * OS + 2 * FEW_ROWS;     // of a wavefront
+    float* const cb0 = (float*)smem;
+    lds_barrier();
+    float* const mine = cb0 + wave * WS;
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float* const mine = cb0 + wave * WS + (c * 32 + rl) * OS;
+    for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-        for (int cb = 0; cb < NCB; ++cb)
+      for (int a = 0; a < 4; ++a)
+        *(floatx4_t*)(mine + rl * OS + cb * 32 + a * 8 + hf * 4) =
+            floatx4_t{o_acc[cb][4 * a], o_acc[cb][4 * a + 1], o_acc[cb][4 * a + 2], o_acc[cb][4 * a + 3]};
+    if (hf == 0) {
+      mine[FEW_ROWS * OS + rl] = m_run;
+      mine[FEW_ROWS * OS + FEW_ROWS + rl] = l_run;
+    }
+    lds_barrier();
+    constexpr int LPR = D / 4, RPI = FEW_WAVES * 64 / LPR;   // lanes of a row, rows at a time
+#pragma unroll 4
+    for (int i = 0; i < FEW_ROWS / RPI; ++i) {
+      const int r = i * RPI + tid / LPR, ch = (tid % LPR) * 4;
+      float m = -INFINITY, l = 0.f;
+      floatx4_t o4 = {0.f, 0.f, 0.f, 0.f};
+      float mw[FEW_WAVES], lw[FEW_WAVES];
+      floatx4_t x[FEW_WAVES];
 #pragma unroll
-          for (int a = 0; a < 4; ++a)
-            *(floatx4_t*)(mine + cb * 32 + a * 8 + hf * 4) =
-                floatx4_t{o_acc[c][cb][4 * a], o_acc[c][cb][4 * a + 1], o_acc[c][cb][4 * a + 2],
-                          o_acc[c][cb][4 * a + 3]};
-        if (hf == 0) {
-          cb0[wave * WS + F::RW * OS + c * 32 + rl] = m_run[c];
-          cb0[wave * WS + F::RW * OS + F::RW + c * 32 + rl] = l_run[c];
-        }
+      for (int w = 0; w < FEW_WAVES; ++w) {
+        mw[w] = cb0[w * WS + FEW_ROWS * OS + r];
+        lw[w] = cb0[w * WS + FEW_ROWS * OS + FEW_ROWS + r];
+        x[w] = *(const floatx4_t*)(cb0 + w * WS + r * OS + ch);
+        m = fmaxf(m, mw[w]);
       }
-      __syncthreads();
-      for (int e = tid; e < F::RW * (D / 4); e += NW * 64) {
-        const int r = e / (D / 4), ch = (e % (D / 4)) * 4;
-        float m = -INFINITY, l = 0.f;
-        floatx4_t o4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < NW; ++w) m = fmaxf(m, cb0[w * WS + F::RW * OS + r]);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-          const float lw = cb0[w * WS + F::RW * OS + F::RW + r];
-          const float f = m == -INFINITY ? lw   // (0, or a NaN)
-                                         : __builtin_amdgcn_exp2f(cb0[w * WS + F::RW * OS + r] - m);
-          const floatx4_t x = *(const floatx4_t*)(cb0 + w * WS + r * OS + ch);
-          l = fmaf(lw, f, l);
-          o4 += x * f;
-        }
-        write(pc.span * F::RM + r, r, m, l, ch, o4);
+      for (int w = 0; w < FEW_WAVES; ++w) {
+        const float f = m == -INFINITY ? lw[w]   // (0, or a NaN)
+                                       : __builtin_amdgcn_exp2f(mw[w] - m);
+        l = fmaf(lw[w], f, l);
+        o4 += x[w] * f;
       }
-      __syncthreads();
-    } else {
-#pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int cb = 0; cb < NCB; ++cb)
-#pragma unroll
-          for (int a = 0; a < 4; ++a)
-            write(row[c], wave * F::RW + c * 32 + rl, m_run[c], l_run[c], cb * 32 + a * 8 + hf * 4,
-                  floatx4_t{o_acc[c][cb][4 * a], o_acc[c][cb][4 * a + 1], o_acc[c][cb][4 * a + 2],
-                            o_acc[c][cb][4 * a + 3]});
+      write(pc.span * FEW_ROWS + r, r, m, l, ch, o4);
     }
     u += t1 - t0;
   }
@@ -664,13 +602,18 @@ __global__ __launch_bounds__(NW * 64) void tree_attn_kernel(const TreeParams p) 
 // ---------------------------------------------------------------------------
 // Many rows (bf16): eight wavefronts with 32 rows each, a tile of 64 keys for all of them.
 //
-// Bound by the matrix pipe and, about as much, by the LDS reads that feed it (a fragment serves 32 rows).
 // A step works on three sub-tiles: the products S^T of the next one and O^T of the one before are issued
-// between the softmax arithmetic of the current one, which needs neither. The reference that the
-// exponentials are taken against is raised only when a score exceeds it by 2^8 (O and the sum are
-// rescaled then): they cancel in O / l, and what is rounded has the same relative error at any scale.
-// A tile travels through registers into one of three LDS buffers: one holds the values of the
-// sub-tile before, one the current tile, and one is being filled; one barrier a tile.
+// between the softmax arithmetic of the current one, which needs neither, and so is the maximum of the
+// next one's scores. The reference that the exponentials are taken against is raised only when a
+// score exceeds it by 2^8 (O and the sum are rescaled then): it cancels in O / l, and what is rounded
+// has the same relative error at any scale.
+// A tile goes straight into one of four LDS buffers: the tile before (its values), the current one, the next
+// and the one being filled; one barrier a tile. (Through registers, with fragments requested four products ahead
+// where now eight fit: 97 and 104 us for 61 nodes of 16 heads over 131072 keys, 88 and 95 for 16 sequences of 2048
+// to 8192 keys with three terms.)
+// Measured: 61 nodes of 16 heads over 131072 keys of one, 94 us, 700 TFLOP/s, of which 75 us are the loop (2050 cycles of
+// a tile's 3900 the matrix pipe), 11 the way to the first product and 5 the parts' way out. No one unit binds the loop:
+// without its LDS reads the call takes 0.92 of the time, without the exponentials 0.98, without the loads 0.92.
 // ---------------------------------------------------------------------------
 constexpr int MANY_WAVES = 8;
 constexpr int MANY_ROWS = 32 * MANY_WAVES;
@@ -688,25 +631,39 @@ __device__ __forceinline__ float halves_max(float x) {
   asm volatile("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
   return fmaxf(a, b);
 }
+// Requests from memory into LDS, 16 or 4 bytes a lane at `dst` (uniform) and on. In assembly: in front of
+// every LDS read the compiler would wait for the requests that it knows of. landed_barrier() waits for them.
+// (No vector register is written. m0 is the compiler's own: it holds nothing across statements, each use sets
+// it. The s_nop is the wait state between its write and its use.)
+__device__ __forceinline__ void dma16(const void* base, uint32_t lane_bytes, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(lane_bytes), "s"(base), "s"(dst) : "memory");
+}
+__device__ __forceinline__ void dma16(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :: "v"(src), "s"(dst) : "memory");
+}
+__device__ __forceinline__ void dma4(const void* src, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+               :: "v"(src), "s"(dst) : "memory");
+}
+// Every wavefront's requests have landed and its LDS reads have returned.
+__device__ __forceinline__ void landed_barrier() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
 // Keeps the computation of x where it is in the instruction stream.
 __device__ __forceinline__ void pin(float& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void pin(u32x4_t& x) { asm volatile("" : "+v"(x)); }
 __device__ __forceinline__ void pin(floatx16_t& x) { asm volatile("" : "+v"(x)); }
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  bf16x2_t t;
-  t[0] = static_cast<bf16_t>(a);
-  t[1] = static_cast<bf16_t>(b);
-  return __builtin_bit_cast(uint32_t, t);
-}
 
 template <int D>
 struct ManyTile {
   using T = SubTile<bf16_t, D>;
-  static constexpr int KEYS = 2 * SUB;
+  static constexpr int KEYS = 2 * SUB;   // (one position a lane of a wavefront)
   static constexpr int V_OFF = KEYS * T::ROW;
   static constexpr int POS_OFF = 2 * KEYS * T::ROW;
   static constexpr int BYTES = POS_OFF + KEYS * 4;
-  static constexpr int ZERO_OFF = 3 * BYTES;           // a sub-tile's worth of V, zeros
+  static constexpr int ZERO_OFF = 4 * BYTES;           // a sub-tile's worth of V, zeros
   static constexpr int SMEM = ZERO_OFF + SUB * T::ROW;
 };
 
@@ -715,7 +672,8 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
   using M = ManyTile<D>;
   using T = SubTile<bf16_t, D>;
   constexpr int NKS = D / 16, NCB = D / 32, NVF = 2 * NCB;
-  constexpr int THREADS = MANY_WAVES * 64, RPI = THREADS / T::CH, CPT = M::KEYS / RPI;
+  constexpr int THREADS = MANY_WAVES * 64;
+  constexpr int RPT = THREADS / T::CH, REQ = M::KEYS / RPT;   // rows of a request of all wavefronts, requests
   static_assert(NKS == NVF, "a V^T fragment takes the registers of a K fragment");
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -723,6 +681,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
   const int rl = lane & 31, hf = lane >> 5;
   for (int i = tid * 16; i < SUB * T::ROW; i += THREADS * 16)
     *(uint4*)(smem + M::ZERO_OFF + i) = make_uint4(0, 0, 0, 0);
+  const int r0 = tid / T::CH, slot = tid % T::CH;   // of a request: row and 16-byte slot in LDS
   int64_t u = 0, u_end = 1;
   const int64_t tok_q = (int64_t)p.n_q_heads * D, tok_kv = (int64_t)p.n_kv_heads * D;
   // LDS offsets of this lane inside a sub-tile: K fragment chunk 2 ks + hf of row rl; V^T fragments
@@ -754,46 +713,50 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
     const int node = sq.q0 + nd;
     const int head = kvh * p.group + (ok ? row - nd * p.group : 0);
 
-    // ---- a tile on its way: K and V rows by 16-byte chunks, positions of the cached ones ----
+    // ---- tiles on their way ----
+    auto buf = [&](int t) { return smem + (t & 3) * M::BYTES; };
     const bf16_t* const kc = (const bf16_t*)p.k + sq.k0 * tok_kv + kvh * D;
     const bf16_t* const vc = (const bf16_t*)p.v + sq.k0 * tok_kv + kvh * D;
-    const bf16_t* const kt = (const bf16_t*)p.k_new + sq.q0 * tok_kv + kvh * D;
-    const bf16_t* const vt = (const bf16_t*)p.v_new + sq.q0 * tok_kv + kvh * D;
-    const bool has_tree = p.k_new != nullptr;
-    static_assert(CPT <= 2, "chunks of a lane");
-    uint4 st_k0, st_k1, st_v0, st_v1;   // (scalars: an array of these ends up in memory)
-    int32_t st_pos = 0;
-    auto fetch_row = [&](int idx, uint4& k, uint4& v) __attribute__((always_inline)) {
-      // (keys behind the last of either kind repeat it, and are masked by their index; a choice between
-      // values, since one between the variables would put them into memory)
-      const bool own = has_tree && idx >= n_cached * SUB;
-      const int key = own ? min(idx - n_cached * SUB, sq.n - 1) : min(idx, sq.used - 1);
-      const int64_t off = key * tok_kv;
-      const bf16_t* const kr = own ? kt + off : kc + off;
-      const bf16_t* const vr = own ? vt + off : vc + off;
-      k = ((const uint4*)kr)[tid % T::CH];
-      v = ((const uint4*)vr)[tid % T::CH];
-    };
-    auto fetch = [&](int t) __attribute__((always_inline)) {
-      fetch_row(t * M::KEYS + tid / T::CH, st_k0, st_v0);
-      if constexpr (CPT > 1) fetch_row(t * M::KEYS + RPI + tid / T::CH, st_k1, st_v1);
-      if (tid < M::KEYS) {
-        const int idx = t * M::KEYS + tid;
-        st_pos = idx < sq.used ? p.kv_pos[sq.k0 + idx] : CP_POS_PAD_KV;
+    // Requests of tile t into `buf`: the wavefront's K and V rows and, the first one, the positions. Keys
+    // behind the last cached or tree's own one repeat it (and are masked by their index).
+    const int k_l = (slot ^ T::k_perm(r0 & 31)) * 8, v_l = (slot ^ T::v_perm(r0 & 31)) * 8;
+    // (32 bits hold a lane's offset inside a tile; of wider rows every address is computed)
+    const bool narrow = tok_kv < (1 << 23);
+    const uint32_t k_lane = ((uint32_t)r0 * (uint32_t)tok_kv + k_l) * 2;
+    const uint32_t v_lane = ((uint32_t)r0 * (uint32_t)tok_kv + v_l) * 2;
+    auto request_tile = [&](int t, const char* buf) __attribute__((always_inline)) {
+      const uint32_t dst = (uint32_t)(size_t)(CP_LDS_AS const char*)buf;
+      const uint32_t at = dst + wave * 1024;
+      const int key0 = t * M::KEYS;
+      if (narrow && key0 + M::KEYS <= sq.used) {   // cached keys alone
+        const int64_t base = key0 * tok_kv;
+#pragma unroll
+        for (int i = 0; i < REQ; ++i) {
+          dma16(kc + (base + i * RPT * tok_kv), k_lane, at + i * RPT * T::ROW);
+          dma16(vc + (base + i * RPT * tok_kv), v_lane, at + i * RPT * T::ROW + M::V_OFF);
+        }
+      } else {
+        const bf16_t* const kt = (const bf16_t*)p.k_new + sq.q0 * tok_kv + kvh * D;
+        const bf16_t* const vt = (const bf16_t*)p.v_new + sq.q0 * tok_kv + kvh * D;
+#pragma unroll
+        for (int i = 0; i < REQ; ++i) {
+          const int idx = key0 + i * RPT + r0;
+          const bool own = p.k_new != nullptr && idx >= n_cached * SUB;
+          const int key = own ? min(idx - n_cached * SUB, sq.n - 1) : min(idx, sq.used - 1);
+          const int64_t off = key * tok_kv;
+          // (a choice between values: one between the variables would put them into memory)
+          dma16((own ? kt + off : kc + off) + k_l, at + i * RPT * T::ROW);
+          dma16((own ? vt + off : vc + off) + v_l, at + i * RPT * T::ROW + M::V_OFF);
+        }
       }
+      if (wave == 0 && sq.used > 0)
+        dma4(p.kv_pos + sq.k0 + min(key0 + lane, sq.used - 1), dst + M::POS_OFF);
     };
-    auto put_row = [&](char* buf, int r, const uint4& k, const uint4& v) __attribute__((always_inline)) {
-      const int c = tid % T::CH;
-      *(uint4*)(buf + r * T::ROW + ((c ^ T::k_perm(r & 31)) << 4)) = k;
-      *(uint4*)(buf + M::V_OFF + r * T::ROW + ((c ^ T::v_perm(r & 31)) << 4)) = v;
-    };
-    auto put = [&](char* buf) __attribute__((always_inline)) {
-      put_row(buf, tid / T::CH, st_k0, st_v0);
-      if constexpr (CPT > 1) put_row(buf, RPI + tid / T::CH, st_k1, st_v1);
-      if (tid < M::KEYS) *(int32_t*)(buf + M::POS_OFF + tid * 4) = st_pos;
-    };
-    if (n_subs > 0) fetch(pc.t0);
-
+    if (n_subs > 0) {
+      lds_barrier();   // the piece before has been read
+      request_tile(pc.t0, buf(pc.t0));
+      if (pc.t0 + 1 < pc.t1) request_tile(pc.t0 + 1, buf(pc.t0 + 1));
+    }
     uint4 qf[NKS];
     const uint4* const q_src = (const uint4*)((const bf16_t*)p.q + node * tok_q + head * D) + hf;
 #pragma unroll
@@ -807,6 +770,8 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
     for (int o = 16; o > 0; o >>= 1) q_min = min(q_min, __shfl_xor(q_min, o, 64));
 
     float ref = -INFINITY, l_run = 0.f;
+    float top = -INFINITY;                 // the next sub-tile's largest score (log2 domain; if it needs no mask)
+    bool masked = false;                   // the next sub-tile needs a mask
     floatx16_t o_acc[NCB], s[2];
     u32x4_t pb[2][TERMS][2];               // P of the current sub-tile and the one before, in bf16 pairs per
                                            // term (keys 0..15, 16..31)
@@ -879,74 +844,89 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
       }
     };
 
-    // One step: softmax of sub-tile st (scores s[PAR], positions at `pos`, values at v_here), products S^T
-    // of the next one (K rows at k_next) and O^T of the one before (V rows at v_prev). Returns whether
-    // the sub-tile's V holds what is not finite and is hidden from a row.
-    auto step = [&](auto parc, int st, const int32_t* pos, const char* v_here, const char* k_next,
-                    const char* v_prev) __attribute__((always_inline)) -> bool {
+    // K fragments 0 .. NKS-1 of the next sub-tile, then V^T fragments of the one before, then K fragments
+    // of the sub-tile after the next: AHEAD of them are on their way
+    constexpr int FRAGS = NKS + NVF, AHEAD = NKS;
+    uint4 fr[AHEAD];
+
+    // Sub-tile st has keys that some row does not see: the tree's own, keys behind the last, or a position
+    // (this lane's `pos`, of key rl) behind a query's.
+    auto needs_mask = [&](int st, int32_t pos) -> bool {   // (cached keys end before the tree's begin)
+      return ((int)(__builtin_amdgcn_ballot_w64(pos > q_min) != 0) | (int)(st * SUB + SUB > sq.used)) != 0;
+    };
+    // Masks the scores s[PAR] of sub-tile st; whether its V holds what is not finite.
+    auto mask = [&](auto parc, int st, const char* sub, const int32_t* pos) __attribute__((always_inline)) -> bool {
       constexpr int PAR = decltype(parc)::value;
-      // K fragments 0 .. NKS-1 of the next sub-tile, then V^T fragments of the one before: AHEAD of them
-      // are on their way
-      constexpr int FRAGS = NKS + NVF, AHEAD = 4;
-      uint4 fr[AHEAD];
-      auto request = [&](int g) __attribute__((always_inline)) {
-        if (g < NKS) fr[g % AHEAD] = k_frag(k_next, g);
-        else if (g < FRAGS) fr[g % AHEAD] = v_frag(v_prev, (g - NKS) % NCB * 2 + (g - NKS) / NCB);
-      };
-#pragma unroll
-      for (int g = 0; g < AHEAD; ++g) request(g);
       const bool own = st >= n_cached;
       const int cnt = own ? sq.n - (st - n_cached) * SUB : sq.used - st * SUB;   // keys, if not SUB
-      bool masked = own || cnt < SUB;
-      if (!masked) masked = __builtin_amdgcn_ballot_w64(pos[rl] > q_min) != 0;
-      uint32_t odd_here = 0;
-      if (masked) {
-        const uint32_t there = st >= n_subs ? 0 : cnt >= SUB ? ~0u : (1u << cnt) - 1;
-        uint32_t see = there;
-        if (own) {
-          const int word = (st - n_cached) >> 1;
-          see = 0;
-          if (ok && word < p.words && there != 0)
-            see = (uint32_t)(p.mask[(int64_t)node * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
-        }
-        see >>= hf * 4;   // (bit a * 8 + i: score 4 a + i)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const int4 x = *(const int4*)(pos + a * 8 + hf * 4);
-          const int32_t kp[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int vis = (int)((see & (1u << (a * 8 + i))) != 0) & ((int)own | (int)(kp[i] <= qp));
-            s[PAR][4 * a + i] = vis != 0 ? s[PAR][4 * a + i] : -INFINITY;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < SUB * T::ROW / 1024; ++i) {
-          const uint4 x = *(const uint4*)(v_here + M::V_OFF + i * 1024 + lane * 16);
-          odd_here |= any_not_finite(x.x) | any_not_finite(x.y) | any_not_finite(x.z) | any_not_finite(x.w);
-        }
-        odd_here = __builtin_amdgcn_ballot_w64(odd_here != 0) != 0;
+      const uint32_t there = st >= n_subs ? 0 : cnt >= SUB ? ~0u : (1u << cnt) - 1;
+      uint32_t see = there;
+      if (own) {
+        const int word = (st - n_cached) >> 1;
+        see = 0;
+        if (ok && word < p.words && there != 0)
+          see = (uint32_t)(p.mask[(int64_t)node * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
       }
+      see >>= hf * 4;   // (bit a * 8 + i: score 4 a + i)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const int4 x = *(const int4*)(pos + a * 8 + hf * 4);
+        const int32_t kp[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int vis = (int)((see & (1u << (a * 8 + i))) != 0) & ((int)own | (int)(kp[i] <= qp));
+          s[PAR][4 * a + i] = vis != 0 ? s[PAR][4 * a + i] : -INFINITY;
+        }
+      }
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < SUB * T::ROW / 1024; ++i) {
+        const uint4 x = *(const uint4*)(sub + M::V_OFF + i * 1024 + lane * 16);
+        odd |= any_not_finite(x.x) | any_not_finite(x.y) | any_not_finite(x.z) | any_not_finite(x.w);
+      }
+      return __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+    };
+    // largest score of the row in s[PAR], log2 domain
+    auto row_max = [&](auto parc) __attribute__((always_inline)) {
+      constexpr int PAR = decltype(parc)::value;
       float mx = fmaxf(fmaxf(s[PAR][0], s[PAR][1]), s[PAR][2]);
 #pragma unroll
       for (int i = 3; i < 15; i += 2) mx = fmaxf(fmaxf(mx, s[PAR][i]), s[PAR][i + 1]);
-      mx = halves_max(fmaxf(mx, s[PAR][15])) * p.scale_log2;
-      const bool raise = mx > ref + kSlack;
+      return halves_max(fmaxf(mx, s[PAR][15])) * p.scale_log2;
+    };
+
+    // One step: softmax of sub-tile st (scores s[PAR], its rows and positions at `sub`, `pos`), products S^T
+    // of the next one (its K fragments on their way, the others at k_next) and O^T of the one before (V rows
+    // at v_prev); the K fragments of the one after the next (k_after) are requested.
+    auto step = [&](auto parc, int st, const char* sub, const int32_t* pos, const char* k_next,
+                    const int32_t* pos_next, const char* k_after, const char* v_prev) __attribute__((always_inline)) {
+      constexpr int PAR = decltype(parc)::value;
+      auto request = [&](int g) __attribute__((always_inline)) {
+        if (g < NKS) fr[g % AHEAD] = k_frag(k_next, g);
+        else if (g < FRAGS) fr[g % AHEAD] = v_frag(v_prev, (g - NKS) % NCB * 2 + (g - NKS) / NCB);
+        else fr[g % AHEAD] = k_frag(k_after, g - FRAGS);
+      };
+      bool odd = false;
+      if (__builtin_expect(masked, 0)) {
+        odd = mask(parc, st, sub, pos);
+        top = row_max(parc);
+      }
+      const bool raise = top > ref + kSlack;
       const bool any_raise = __builtin_amdgcn_ballot_w64(raise) != 0;
       float alpha = 1.f;
-      if (any_raise) {
+      if (__builtin_expect(any_raise, 0)) {
         if (raise) {
-          alpha = __builtin_amdgcn_exp2f(ref - mx);
-          ref = mx;
+          alpha = __builtin_amdgcn_exp2f(ref - top);
+          ref = top;
         }
         l_run *= alpha;
       }
-      const float use = ref == -INFINITY ? 0.f : ref;
 
       // Softmax arithmetic in units, two MFMA slots or so apart: argument of score w, exponential of the
       // one before, sum and rounding of the one before that.
-      constexpr int UNITS = 18, SLOTS = NKS + NVF * TERMS;
-      float e[16], sum[2] = {0.f, 0.f};
+      constexpr int UNITS = 18, SLOTS = NKS + NVF * TERMS, MAX_SLOTS = SLOTS - NKS - 2 >= 4 ? 4 : 2;
+      const float use = ref == -INFINITY ? 0.f : ref;
+      float e[16], sum[2] = {0.f, 0.f}, mx = -INFINITY;
       auto unit = [&](int w) __attribute__((always_inline)) {
         if (w >= 2) {
           const int i = w - 2;
@@ -965,9 +945,17 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
         if (w >= 1 && w < 17) e[w - 1] = __builtin_amdgcn_exp2f(e[w - 1]);
         if (w < 16) e[w] = fmaf(s[PAR][w], p.scale_log2, -use);
       };
+      int32_t next_pos = 0;
       auto units = [&](int slot) __attribute__((always_inline)) {
+        if (slot == 1) next_pos = pos_next[rl];
 #pragma unroll
         for (int w = slot * UNITS / SLOTS; w < (slot + 1) * UNITS / SLOTS; ++w) unit(w);
+        // the largest score of the next sub-tile, whose products are complete two slots after their last
+        if (slot >= NKS + 2 && slot < NKS + 2 + MAX_SLOTS) {
+          const int i0 = (slot - NKS - 2) * (16 / MAX_SLOTS);
+#pragma unroll
+          for (int i = i0; i < i0 + 16 / MAX_SLOTS; i += 2) mx = fmaxf(fmaxf(mx, s[PAR ^ 1][i]), s[PAR ^ 1][i + 1]);
+        }
         __builtin_amdgcn_sched_barrier(0);
       };
 #pragma unroll
@@ -990,60 +978,59 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
           }
         }
       }
-      l_run += sum[0] + sum[1];
       // (all of this belongs in front of the branch below: the optimiser would sink it behind it)
       pin(s[PAR ^ 1]);
+      l_run += sum[0] + sum[1];
       pin(l_run);
+      top = halves_max(mx) * p.scale_log2;
 #pragma unroll
       for (int k = 0; k < TERMS; ++k)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) pin(pb[PAR][k][kb]);
 #pragma unroll
       for (int cb = 0; cb < NCB; ++cb) pin(o_acc[cb]);
-      if (any_raise) {
+      masked = needs_mask(st + 1, next_pos);
+      if (__builtin_expect(any_raise, 0)) {
 #pragma unroll
         for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
           for (int i = 0; i < 16; ++i) o_acc[cb][i] *= alpha;
       }
-      return odd_here != 0;
-    };
-    auto run_step = [&](auto parc, int st, const int32_t* pos, const char* v_here, const char* k_next,
-                        const char* v_prev) __attribute__((always_inline)) {
-      // (no product is pending: P times zeros)
-      const bool odd = step(parc, st, pos, v_here, k_next, pending ? v_prev : smem + M::ZERO_OFF - M::V_OFF);
-      if (__builtin_expect(odd, 0)) value_product(parc, IntC<1>{}, v_here);
+      if (__builtin_expect(odd, 0)) value_product(parc, IntC<1>{}, sub);
       pending = !odd;
     };
 
     if (n_subs > 0) {
       constexpr int HALF = SUB * T::ROW;   // bytes from a tile's first sub-tile to its second
-      char *prev = smem, *cur = smem + M::BYTES, *next = smem + 2 * M::BYTES;
-      lds_barrier();   // the piece before has been read
-      put(cur);
-      if (pc.t0 + 1 < pc.t1) fetch(pc.t0 + 1);
-      lds_barrier();
+      auto pos_of = [](const char* b) { return (const int32_t*)(b + M::POS_OFF); };
+      landed_barrier();
+      if (pc.t0 + 2 < pc.t1) request_tile(pc.t0 + 2, buf(pc.t0 + 2));
+      {
+        const char* const b = buf(pc.t0);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+        for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
 #pragma unroll
-      for (int ks = 0; ks < NKS; ++ks)
-        s[0] = mfma32(__builtin_bit_cast(bf16x8_t, k_frag(cur, ks)), __builtin_bit_cast(bf16x8_t, qf[ks]), s[0]);
-      for (int t = pc.t0; t < pc.t1; ++t) {
-        const int32_t* const pos = (const int32_t*)(cur + M::POS_OFF);
-        run_step(IntC<0>{}, 2 * t, pos, cur, cur + HALF, prev + HALF);
-        if (t + 1 < pc.t1) {
-          put(next);
-          if (t + 2 < pc.t1) fetch(t + 2);
-        }
-        lds_barrier();
-        // (a second sub-tile that is not there holds copies of the last key, none of which counts)
-        run_step(IntC<1>{}, 2 * t + 1, pos + SUB, cur + HALF, next, cur);
-        char* const x = prev;
-        prev = cur;
-        cur = next;
-        next = x;
+        for (int ks = 0; ks < NKS; ++ks)
+          s[0] = mfma32(__builtin_bit_cast(bf16x8_t, k_frag(b, ks)), __builtin_bit_cast(bf16x8_t, qf[ks]), s[0]);
+#pragma unroll
+        for (int g = 0; g < AHEAD; ++g) fr[g] = k_frag(b + HALF, g);
+        masked = needs_mask(2 * pc.t0, pos_of(b)[rl]);
+        top = row_max(IntC<0>{});
       }
-      if (pending) value_product(IntC<1>{}, IntC<0>{}, prev + HALF);
+      const char* const zeros = smem + M::ZERO_OFF - M::V_OFF;   // (no product is pending: P times zeros)
+      for (int t = pc.t0; t < pc.t1; ++t) {
+        const char* const b = buf(t);
+        const char* const b_next = buf(t + 1);
+        step(IntC<0>{}, 2 * t, b, pos_of(b), b + HALF, pos_of(b) + SUB, b_next,
+             pending ? buf(t - 1) + HALF : zeros);
+        // (the next tile but one has landed everywhere, and the values of the one before have been read)
+        landed_barrier();
+        if (t + 3 < pc.t1) request_tile(t + 3, buf(t + 3));
+        // (a second sub-tile that is not there holds copies of the last key, none of which counts)
+        step(IntC<1>{}, 2 * t + 1, b + HALF, pos_of(b) + SUB, b_next, pos_of(b_next), b_next + HALF,
+             pending ? b : zeros);
+      }
+      if (pending) value_product(IntC<1>{}, IntC<0>{}, buf(pc.t1 - 1) + HALF);
     }
     l_run += xor32(l_run);
 
@@ -1079,14 +1066,16 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
   }
 }
 
-// Joins the parts of the spans that fell into several shares, a wavefront per row: lane l knows the
-// maximum and sum of part l, and the rows of eight parts are in flight at a time.
-template <int D, int RM, int SPT, typename TO>
+// Joins the parts of the spans that fell into several shares, W wavefronts per row: lane l knows the
+// maximum and sum of its wavefront's part l, and the rows of eight parts are in flight at a time. Bound by the
+// parts' bytes where there are many rows (10 us for 33 MB); few rows (and so, many parts of each) take four
+// wavefronts each: 9.1 us instead of 10.7 for 976 rows in 64 parts.
+template <int D, int RM, int SPT, int W, typename TO>
 __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
-  constexpr int V = D / 64, U = 8;
+  constexpr int V = D / 64, U = 8, CHUNK = 64 / W;
   typedef float vec_t __attribute__((ext_vector_type(V)));
-  const int lane = threadIdx.x & 63;
-  const int64_t idx = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t idx = (int64_t)blockIdx.x * (4 / W) + wave / W;
   if (idx >= p.total_q * p.n_q_heads) return;
   const int node = (uint32_t)idx / (uint32_t)p.n_q_heads;
   const int head = (int)idx - node * p.n_q_heads, kvh = (uint32_t)head / (uint32_t)p.group;
@@ -1101,11 +1090,13 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
   const int n = (int)div64((uint64_t)(a + sq.tiles - 1), (uint32_t)line.share) - w0 + 1;
   if (n == 1) return;
   // (the first part begins the span)
-  auto at = [&](int k) { return (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * RM + (row - span * RM); };
+  auto at = [&](int k) __attribute__((always_inline)) {
+    return (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * RM + (row - span * RM);
+  };
   float m = -INFINITY, l = 0.f;
   vec_t o = {};
-  for (int k0 = 0; k0 < n; k0 += 64) {
-    const int cnt = min(64, n - k0);
+  for (int k0 = wave % W * CHUNK; k0 < n; k0 += 64) {
+    const int cnt = min(CHUNK, n - k0);
     float mw = -INFINITY, lw = 0.f;
     if (lane < cnt) {
       const float2 x = *(const float2*)(p.part_ml + at(k0 + lane) * 2);
@@ -1113,22 +1104,22 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
       lw = x.y;
     }
     vec_t x[U];
-    auto rows = [&](int k) {
+    auto rows = [&](int k) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < U; ++u) x[u] = *(const vec_t*)(p.part_o + at(k0 + min(k + u, cnt - 1)) * D + lane * V);
     };
     rows(0);
     float top = mw;
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, 64));
-    const float mn = fmaxf(m, top);
+    for (int s = CHUNK / 2; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, CHUNK));
+    const float mn = fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, top))));
     const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
     // (a part that saw nothing has weight 0; one that saw a NaN alone has no maximum and that sum)
     const float f = lw == 0.f ? 0.f : mw == -INFINITY ? lw : __builtin_amdgcn_exp2f(mw - mn);
     float sum = lw * f;
 #pragma unroll
-    for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s, 64);
-    l = fmaf(l, old, sum);
+    for (int s = CHUNK / 2; s > 0; s >>= 1) sum += __shfl_xor(sum, s, CHUNK);
+    l = fmaf(l, old, __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, sum))));
     m = mn;
     o *= old;
     for (int k = 0; k < cnt; k += U) {
@@ -1140,6 +1131,26 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
         if (k + u < cnt) o += x[u] * fu;
       }
     }
+  }
+  if constexpr (W > 1) {   // (all of a workgroup's wavefronts have come this far: one row)
+    __shared__ vec_t other[W][64];
+    __shared__ float2 ml[W];
+    other[wave][lane] = o;
+    if (lane == 0) ml[wave] = make_float2(m, l);
+    __syncthreads();
+    if (wave > 0) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, ml[w].x);
+    l = 0.f;
+    o = vec_t{};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = ml[w].y == 0.f ? 0.f : ml[w].x == -INFINITY ? ml[w].y : __builtin_amdgcn_exp2f(ml[w].x - top);
+      l = fmaf(ml[w].y, f, l);
+      o += other[w][lane] * f;
+    }
+    m = top;
   }
   const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
   o *= inv;
@@ -1215,24 +1226,30 @@ __global__ __launch_bounds__(ACCEPT_THREADS) void tree_accept_kernel(const Accep
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-enum TreeForm { kFew32, kFew64, kMany };
+constexpr int64_t kFewProducts = 1 << 19;
 struct TreePlan {
-  TreeForm form;
-  int rm, spt, n_wg, log2_wg, min_share;
+  bool many;
+  int rm, spt, n_wg, log2_wg;
   size_t o_bytes, ml_bytes;
 };
 TreePlan tree_plan(const cp_shape& s) {
   TreePlan pl = {};
   const int64_t group = s.n_q_heads / s.n_kv_heads;
-  const int64_t rows = s.total_q * group / s.batch;   // of a sequence, on average
-  pl.form = s.dtype == CP_FP32 || rows <= 32 ? kFew32 : rows <= 128 ? kFew64 : kMany;
-  pl.rm = pl.form == kFew32 ? 32 : pl.form == kFew64 ? 64 : MANY_ROWS;
-  pl.spt = pl.form == kMany ? 2 : 4;
-  pl.min_share = 1;
+  // Rows of a sequence on average, and 32-row blocks times sub-tiles of all: the form for many rows reads a
+  // key once for 256 rows and has three times the matrix rate, the other starts and ends sooner. us (few rows,
+  // many): head_dim 128, 16 heads on one, 4096 keys: 8 sequences of 32 rows 21.7 and 24.6, of 128 30.0 and
+  // 31.0, of 192 37.7 and 34.8; 32 sequences of 32 rows 29.7 and 37.0, of 64 42.7 and 38.9, of 256 99 and 53;
+  // 1 sequence of 8192 keys, 384 rows 31.5 and 34.1. Head_dim 64, 8 heads on two: 8 sequences of 64 rows 16.6 and 20.4, of
+  // 128 23.6 and 23.2; 32 sequences of 32 rows 23.6 and 39.0, of 128 54.8 and 43.7.
+  const int64_t rows = s.total_q * group / s.batch;
+  const int64_t subs = ((s.total_kv + s.total_q) / SUB + s.batch) * s.n_kv_heads;
+  pl.many = s.dtype == CP_BF16 && rows > 32 && subs > kFewProducts / s.head_dim / ((rows + 31) / 32);
+  pl.rm = pl.many ? MANY_ROWS : FEW_ROWS;
+  pl.spt = pl.many ? 2 : FEW_WAVES;
   // no more workgroups than there can be tiles
   const int64_t spans = s.total_q * group / pl.rm + s.batch;
   const int64_t tiles = (s.total_kv + s.total_q) / (SUB * pl.spt) + 2 * (int64_t)s.batch;
-  const int64_t most = pl.form == kMany ? 256 : 512;
+  const int64_t most = pl.many ? 256 : 512;
   const int64_t any = spans > most || tiles > most ? most : spans * tiles * s.n_kv_heads;
   while ((1 << pl.log2_wg) < any && (1 << pl.log2_wg) < most) ++pl.log2_wg;
   pl.n_wg = 1 << pl.log2_wg;
@@ -1241,21 +1258,28 @@ TreePlan tree_plan(const cp_shape& s) {
   return pl;
 }
 
-template <typename TI, int D, bool KS, int C, int NW, int TERMS, typename TO>
-int launch_form(const TreeParams& p, hipStream_t st) {
-  using F = Form<KS, C, NW>;
-  constexpr int smem = tree_smem<TI, D, KS, C, NW>();
+constexpr int64_t kJoinRows = 2048;   // (four wavefronts a row fill the card's 8192 places)
+template <int D, int RM, int SPT, typename TO>
+int launch_join(const TreeParams& p, hipStream_t st) {
+  const int64_t rows = p.total_q * p.n_q_heads;
+  if (rows <= kJoinRows)
+    hipLaunchKernelGGL((tree_join_kernel<D, RM, SPT, 4, TO>), dim3((unsigned)rows), dim3(256), 0, st, p);
+  else
+    hipLaunchKernelGGL((tree_join_kernel<D, RM, SPT, 1, TO>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
+  return check_launch();
+}
+
+template <typename TI, int D, int TERMS, typename TO>
+int launch_few(const TreeParams& p, hipStream_t st) {
+  constexpr int smem = few_smem<TI, D>();
   static_assert(smem <= 160 * 1024, "LDS of a CU");
-  auto kernel = tree_attn_kernel<TI, D, KS, C, NW, TERMS, TO>;
+  auto kernel = tree_few_kernel<TI, D, TERMS, TO>;
   if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, smem) !=
       hipSuccess)
     return CP_ERR_LAUNCH;
-  hipLaunchKernelGGL(kernel, dim3(p.n_wg), dim3(NW * 64), smem, st, p);
+  hipLaunchKernelGGL(kernel, dim3(p.n_wg), dim3(FEW_WAVES * 64), smem, st, p);
   if (check_launch() != CP_OK) return CP_ERR_LAUNCH;
-  const int64_t rows = p.total_q * p.n_q_heads;
-  hipLaunchKernelGGL((tree_join_kernel<D, F::RM, F::SPT, TO>), dim3((unsigned)((rows + 3) / 4)),
-                     dim3(256), 0, st, p);
-  return check_launch();
+  return launch_join<D, FEW_ROWS, FEW_WAVES, TO>(p, st);
 }
 
 template <int D, int TERMS, typename TO>
@@ -1267,19 +1291,12 @@ int launch_many(const TreeParams& p, hipStream_t st) {
     return CP_ERR_LAUNCH;
   hipLaunchKernelGGL(kernel, dim3(p.n_wg), dim3(MANY_WAVES * 64), ManyTile<D>::SMEM, st, p);
   if (check_launch() != CP_OK) return CP_ERR_LAUNCH;
-  const int64_t rows = p.total_q * p.n_q_heads;
-  hipLaunchKernelGGL((tree_join_kernel<D, MANY_ROWS, 2, TO>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st,
-                     p);
-  return check_launch();
+  return launch_join<D, MANY_ROWS, 2, TO>(p, st);
 }
 
 template <int D, int TERMS, typename TO>
-int launch_bf16(const TreeParams& p, TreeForm form, hipStream_t st) {
-  switch (form) {
-    case kFew32: return launch_form<bf16_t, D, true, 1, 4, TERMS, TO>(p, st);
-    case kFew64: return launch_form<bf16_t, D, true, 2, 4, TERMS, TO>(p, st);
-    default: return launch_many<D, TERMS, TO>(p, st);
-  }
+int launch_bf16(const TreeParams& p, bool many, hipStream_t st) {
+  return many ? launch_many<D, TERMS, TO>(p, st) : launch_few<bf16_t, D, TERMS, TO>(p, st);
 }
 
 }  // namespace
@@ -1362,20 +1379,20 @@ int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
   p.part_ml = (float*)((char*)workspace + pl.o_bytes);
   p.total_q = s.total_q; p.total_kv = s.total_kv; p.batch = s.batch;
   p.n_q_heads = s.n_q_heads; p.n_kv_heads = s.n_kv_heads; p.group = s.n_q_heads / s.n_kv_heads;
-  p.n_wg = pl.n_wg; p.log2_wg = pl.log2_wg; p.min_share = pl.min_share;
+  p.n_wg = pl.n_wg; p.log2_wg = pl.log2_wg;
   p.scale_log2 = (s.softmax_scale > 0.f ? s.softmax_scale : 1.0f / sqrtf((float)s.head_dim)) * kLog2e;
   hipStream_t st = (hipStream_t)stream;
   const bool f32_out = out_dtype == CP_FP32;
   if (s.dtype == CP_FP32) {
     if (s.head_dim == 64)
-      return f32_out ? launch_form<float, 64, true, 1, 4, 1, float>(p, st)
-                     : launch_form<float, 64, true, 1, 4, 1, bf16_t>(p, st);
-    return f32_out ? launch_form<float, 128, true, 1, 4, 1, float>(p, st)
-                   : launch_form<float, 128, true, 1, 4, 1, bf16_t>(p, st);
+      return f32_out ? launch_few<float, 64, 1, float>(p, st)
+                     : launch_few<float, 64, 1, bf16_t>(p, st);
+    return f32_out ? launch_few<float, 128, 1, float>(p, st)
+                   : launch_few<float, 128, 1, bf16_t>(p, st);
   }
   if (s.head_dim == 64)
-    return f32_out ? launch_bf16<64, 3, float>(p, pl.form, st) : launch_bf16<64, 1, bf16_t>(p, pl.form, st);
-  return f32_out ? launch_bf16<128, 3, float>(p, pl.form, st) : launch_bf16<128, 1, bf16_t>(p, pl.form, st);
+    return f32_out ? launch_bf16<64, 3, float>(p, pl.many, st) : launch_bf16<64, 1, bf16_t>(p, pl.many, st);
+  return f32_out ? launch_bf16<128, 3, float>(p, pl.many, st) : launch_bf16<128, 1, bf16_t>(p, pl.many, st);
 }
 
 int cp_tree_accept(const cp_shape* shape, const void* k_new, const void* v_new,
