@@ -167,9 +167,9 @@ template <int RM, int SPT>
 __device__ __forceinline__ bool tree_piece(TreeLine<RM, SPT>& line, int64_t u, int64_t u_end, TreePiece* x) {
   int64_t v = u, begin;
   x->kvh = 0;
-  while (v >= line.head_tiles) {
-    v -= line.head_tiles;
-    ++x->kvh;
+  if (v >= line.head_tiles) {
+    x->kvh = ((v | line.head_tiles) >> 32) == 0 ? (uint32_t)v / (uint32_t)line.head_tiles : (int)(v / line.head_tiles);
+    v -= x->kvh * line.head_tiles;
   }
   if (line.find(v, &begin, &x->sq) < 0) return false;
   const int64_t in = v - begin;

@@ -56,6 +56,15 @@ TREES = {
     "d64": ([333, 64, 65], [12, 33, 64], 8, 2, 64, "bf16"),
     "d64_rows": ([600], [100], 32, 2, 64, "bf16"),
     "d64_few": ([600, 1200], [1, 2], 8, 1, 64, "bf16"),
+    # enough products for the form that takes 256 rows at a time: its edges, more than 64 sequences with
+    # several to a workgroup, odd groups and counts of sub-tiles, one row block and a row more
+    "m_edges": ([9991, 33, 0, 64, 63], [61, 16, 17, 1, 40], 16, 1, 128, "bf16"),
+    "m_seqs": ([700 + 97 * (i % 17) if i % 9 else 0 for i in range(100)], [5 + 5 * (i % 4) if i % 7 else 0 for i in range(100)],
+               8, 2, 128, "bf16"),
+    "m_odd_group": ([2500, 31], [131, 130], 15, 3, 128, "bf16"),
+    "m_one_more": ([16417], [257], 2, 2, 128, "bf16"),
+    "m_d64": ([3303, 700], [100, 61], 32, 2, 64, "bf16"),
+    "m_d64_seqs": ([500 + 131 * (i % 7) for i in range(70)], [9 + i % 8 for i in range(70)], 8, 2, 64, "bf16"),
     "fp32": ([200, 0, 333], [5, 33, 66], 4, 1, 64, "fp32"),
     "fp32_128": ([200, 129], [9, 2], 6, 2, 128, "fp32"),
 }
@@ -73,7 +82,61 @@ def test_tree_attention(name, out_dtype):
     check_tree(got, reference(x, host, own=False), d, out_dtype, dtype == "bf16" and out_dtype == BF16, name)
 
 
-@pytest.mark.parametrize("name", ["edges", "rows", "chat", "d64", "fp32"])
+def test_which_trees_have_many_rows():
+    # (the workspace holds two row blocks of parts a workgroup)
+    for name, (lens, nodes, nh, nkv, d, dtype) in TREES.items():
+        s = B.make_shape(B.CP_BF16 if dtype == "bf16" else B.CP_FP32, d, nh, nkv, sum(nodes), sum(lens) + 40 * len(lens),
+                         len(lens))
+        few = 2 * 512 * 32 * (d + 2) * 4 + 512
+        assert (B.cp_workspace_bytes(s, B.CP_WS_TREE) > few) == name.startswith("m_"), name
+
+
+@pytest.mark.parametrize("out_dtype", [BF16, F32])
+@pytest.mark.parametrize("name", ["chat", "long", "d64", "fp32", "m_edges", "m_odd_group", "m_d64", "m_seqs"])
+def test_scores_that_keep_growing(name, out_dtype):
+    """The running maximum rises all the way along the cache, in the tree, and by hundreds at single keys."""
+    lens, nodes, nh, nkv, d, dtype = TREES[name]
+    cache, host = make_cache(61, lens, [n + 5 for n in lens], nkv, d, dtype)
+    x = tree_inputs(62, lens, nodes, nh, nkv, d, dtype)
+    grow = np.ones(cache.slots)
+    for b, n in enumerate(lens):
+        lo = host["cu"][b]
+        grow[lo:lo + n] = np.linspace(0.1, 9.0, n)
+        grow[lo + n // 3:lo + n:997] = 60.0
+    k = (cache.k.double().cpu() * torch.as_tensor(grow)[:, None, None]).to(cache.k.dtype)
+    cache.k.copy_(k)
+    host["k"] = k.double().numpy()
+    x["k"] = (x["k"].double() * 10).to(x["k"].dtype)
+    x["k64"] = x["k"].double().numpy()
+    check_tree(run_tree(cache, x, out_dtype), reference(x, host), d, out_dtype, dtype == "bf16" and out_dtype == BF16, name)
+
+
+def test_rows_too_wide_for_offsets_of_32_bits():
+    # 65536 KV heads: the rows of a tile lie up to 500 MB apart
+    nkv, group, d, n, t = 65536, 17, 128, 70, 2
+    free, _ = torch.cuda.mem_get_info()
+    if free < 20 << 30:
+        pytest.skip("16 GB of tensors")
+    cache = B.KVCache([n], nkv, d)
+    g = torch.Generator(device="cuda").manual_seed(71)
+    rand = lambda *s: torch.randn(s, device="cuda", dtype=BF16, generator=g)
+    cache.k.copy_(rand(n, nkv, d))
+    cache.v.copy_(rand(n, nkv, d))
+    cache.kv_pos.copy_(torch.arange(n, dtype=torch.int32))
+    cache.used.copy_(i32([n, 0]))
+    q, k, v = rand(t, nkv * group, d), rand(t, nkv, d), rand(t, nkv, d)
+    q_pos, cu, mask = np.array([40, n], dtype=np.int32), ends([t]), np.array([[1], [3]], dtype=np.int64)
+    got = B.cp_tree_attn(cache, q, i32(q_pos), k, v, i32(cu), dev(torch.as_tensor(mask)), out_dtype=F32)
+    some = [0, 1, 32767, 40000, 65535]
+    at = torch.as_tensor(some).cuda()
+    rows = (at[:, None] * group + torch.arange(group, device="cuda")).reshape(-1)
+    h64 = lambda a, i: a[:, i].double().cpu().numpy()
+    host = dict(k=h64(cache.k, at), v=h64(cache.v, at), kv_pos=np.arange(n), used=[n], cu=[0, n])
+    ref = tree_reference(h64(q, rows), q_pos, cu, host, h64(k, at), h64(v, at), mask)
+    check_tree((got[0][:, rows], got[1][:, rows]), ref, d, F32, False)
+
+
+@pytest.mark.parametrize("name", ["edges", "rows", "chat", "d64", "fp32", "m_edges", "m_odd_group", "m_d64"])
 def test_tree_masks_that_are_no_trees(name):
     """Any bits, bits of nodes that are not there, rows without any; positions in any order that hide
     part of the cache, all of it (padded queries) or padded tokens of it."""
@@ -104,7 +167,7 @@ def test_tree_wider_than_its_words():
     check_tree(run_tree(cache, x, F32), reference(x, host), 128, F32, False)
 
 
-@pytest.mark.parametrize("name", ["chat", "rows", "d64", "d64_few", "fp32"])
+@pytest.mark.parametrize("name", ["chat", "rows", "d64", "d64_few", "fp32", "m_edges", "m_odd_group", "m_d64", "m_d64_seqs"])
 def test_hidden_rows_that_are_not_finite(name):
     """What a node does not see does not reach it: bit by bit the same rows with NaN and infinity in
     hidden K and V rows, of the cache, of other nodes, and in the rows of other queries."""
@@ -582,3 +645,33 @@ def test_same_inputs_same_bits():
     for _ in range(5):
         assert all(torch.equal(a, b) for a, b in zip(run_tree(cache, x, BF16), first))
         assert torch.equal(w(), w0)
+
+
+def test_trees_of_many_rows_in_a_graph():
+    """Replayed with eager calls on the same workspace in between: bit by bit the eager result each time."""
+    lens, nodes, nh, nkv, d, dtype = TREES["m_edges"]
+    cache, _ = make_cache(161, lens, [n + 64 for n in lens], nkv, d)
+    x = tree_inputs(162, lens, nodes, nh, nkv, d, dtype)
+    other = tree_inputs(163, lens, nodes, nh, nkv, d, dtype)
+    s = B.make_shape(B.CP_BF16, d, nh, nkv, len(x["q_pos"]), cache.slots, len(lens))
+    ws = torch.empty(B.cp_workspace_bytes(s, B.CP_WS_TREE), dtype=torch.uint8, device="cuda")
+    args = [dev(x["q"]), i32(x["q_pos"]), dev(x["k"]), dev(x["v"]), i32(x["cu"]), dev(x["mask"])]
+    want = B.cp_tree_attn(cache, *args, out_dtype=BF16, workspace=ws)
+    want = [t.clone() for t in want]
+    out, lse = torch.empty_like(want[0]), torch.empty_like(want[1])
+    step = lambda: B.cp_tree_attn(cache, *args, out=out, lse=lse, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(4):
+        out.fill_(7), lse.fill_(7)
+        run_tree(cache, other, BF16, workspace=ws)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
