@@ -61,6 +61,7 @@ struct TreeParams {
 struct TreeSeq {
   int32_t q0, n, k0, used;   // first node, nodes, first cache slot, tokens in the cache
   int32_t spans, tiles;      // row blocks of a KV head, tiles of each
+  int32_t parts;             // of each, where every workgroup takes one
   __device__ __forceinline__ TreeSeq of_lane(int l) const {
     TreeSeq r;
     r.q0 = __builtin_amdgcn_readlane(q0, l);
@@ -69,6 +70,7 @@ struct TreeSeq {
     r.used = __builtin_amdgcn_readlane(used, l);
     r.spans = __builtin_amdgcn_readlane(spans, l);
     r.tiles = __builtin_amdgcn_readlane(tiles, l);
+    r.parts = __builtin_amdgcn_readlane(parts, l);
     return r;
   }
   __device__ __forceinline__ int cached_subs() const { return (used + SUB - 1) / SUB; }
@@ -89,13 +91,21 @@ __device__ __forceinline__ uint32_t div64(uint64_t a, uint32_t b) {   // quotien
 // The line of all tiles: KV heads, in each the sequences, in each the row blocks (RM rows), in each the
 // tiles (SPT sub-tiles). Up to 64 sequences are described by one round trip, a lane each; of more, the
 // lanes hold 64 at a time.
+// It is cut into equal shares wherever they end, or, where there are few spans, so that no share
+// has tiles of two: a span takes as many workgroups as it needs at `share` tiles each. A workgroup with a second
+// piece (its Q, first tiles and result anew) is done as late as one with kPiece tiles more. us, anywhere and at spans'
+// ends: 61 nodes of 16 heads over 131072 keys 99.8 and 90.3, 16 sequences of 2048 to 8192 keys 70.9 and 66.4, 64 of 500 to
+// 4000 64.1 and 56.1, 8 of 900 to 6000 with head_dim 64 38.4 and 33.7, 32 of 1000 to 8000 with two nodes 34.2 and 29.2.
 template <int RM, int SPT>
 struct TreeLine {
+  static constexpr int kPiece = SPT == 2 ? 8 : 4;
   const TreeParams& p;
   TreeSeq mine;
-  int64_t end;        // tiles of the sequences up to the lane's, of those held
+  int64_t end;        // units (tiles, or parts) of the sequences up to the lane's, of those held
   int held;           // first of the sequences held
-  int64_t head_tiles, share;
+  int64_t head_units; // of a KV head
+  int64_t share;      // tiles
+  bool single;        // a part each
 
   __device__ __forceinline__ void hold(int b0) {
     held = b0;
@@ -107,20 +117,55 @@ struct TreeLine {
     mine.k0 = (int32_t)clamp64(c0, 0, p.total_kv);
     mine.used = (int32_t)clamp64(u, 0, clamp64(c1, mine.k0, p.total_kv) - mine.k0);
     mine.spans = (mine.n * p.group + RM - 1) / RM;   // (rows of a KV head in 31 bits: the host checks)
+    if (b0 + (int)(threadIdx.x & 63) >= p.batch) mine.spans = 0;
     const int subs = mine.cached_subs() + (p.k_new != nullptr ? (mine.n + SUB - 1) / SUB : 0);
     mine.tiles = subs > 0 ? (subs + SPT - 1) / SPT : 1;   // (nothing to see: one tile, empty)
-    end = wave_scan64(b0 + (int)(threadIdx.x & 63) < p.batch ? (int64_t)mine.spans * mine.tiles : 0);
+    mine.parts = 0;
+    if (single) cut();
+    else end = wave_scan64((int64_t)mine.spans * mine.tiles);
+  }
+  __device__ __forceinline__ void cut() {
+    mine.parts = ((uint32_t)mine.tiles + (uint32_t)share - 1) / (uint32_t)share;
+    end = wave_scan64((int64_t)mine.spans * mine.parts);
   }
   __device__ __forceinline__ explicit TreeLine(const TreeParams& params) : p(params) {
-    head_tiles = 0;
+    single = false;
+    head_units = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 64) {
       hold(b0);
-      head_tiles += readlane64(end, 63);
+      head_units += readlane64(end, 63);
     }
-    const int64_t all = head_tiles * p.n_kv_heads;
+    const int64_t all = head_units * p.n_kv_heads;
     share = (all + p.n_wg - 1) >> p.log2_wg;
+    if (share == 1) return;   // (no share has two pieces)
+    int64_t spans = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      if (b0 != held) hold(b0);
+      spans += readlane64(wave_scan64(mine.spans), 63);
+    }
+    spans *= p.n_kv_heads;
+    if (2 * spans > p.n_wg) return;
+    const int64_t one = div64((uint64_t)(all + p.n_wg - spans - 1), (uint32_t)(p.n_wg - spans));
+    if (one > share + kPiece) return;
+    single = true;            // (n_wg - spans + spans parts at most)
+    share = one;
+    head_units = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 64) {
+      if (b0 != held) hold(b0);
+      else cut();
+      head_units += readlane64(end, 63);
+    }
   }
-  // The sequence of tile u of a KV head (-1: behind the last), and the tile where it begins.
+  // The units of a workgroup.
+  __device__ __forceinline__ void mine_to_do(int64_t* u, int64_t* u_end) const {
+    const int64_t each = single ? 1 : share;
+    *u = blockIdx.x * each;
+    *u_end = min(head_units * p.n_kv_heads, *u + each);
+  }
+  __device__ __forceinline__ int64_t units(const TreeSeq& sq) const {
+    return (int64_t)sq.spans * (single ? sq.parts : sq.tiles);
+  }
+  // The sequence of unit u of a KV head (-1: behind the last), and the unit where it begins.
   __device__ __forceinline__ int find(int64_t u, int64_t* begin, TreeSeq* sq) {
     int64_t base = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 64) {
@@ -129,14 +174,14 @@ struct TreeLine {
       if (behind != 0) {
         const int l = __builtin_ctzll(behind);
         *sq = mine.of_lane(l);
-        *begin = base + readlane64(end, l) - (int64_t)sq->spans * sq->tiles;
+        *begin = base + readlane64(end, l) - units(*sq);
         return b0 + l;
       }
       base += readlane64(end, 63);
     }
     return -1;
   }
-  // The sequence that node t belongs to (-1: behind the last tree), and the tiles before it.
+  // The sequence that node t belongs to (-1: behind the last tree), and the units before it.
   __device__ __forceinline__ int find_node(int t, int64_t* begin, TreeSeq* sq) {
     int64_t base = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 64) {
@@ -146,7 +191,7 @@ struct TreeLine {
       if (hit != 0) {
         const int l = __builtin_ctzll(hit);
         *sq = mine.of_lane(l);
-        *begin = base + readlane64(end, l) - (int64_t)sq->spans * sq->tiles;
+        *begin = base + readlane64(end, l) - units(*sq);
         return b0 + l;
       }
       base += readlane64(end, 63);
@@ -162,25 +207,38 @@ struct TreePiece {
   int n_cached, n_subs;
   bool whole;        // the span is all in this piece: its result goes to the output
   int slot;          // otherwise: where the part goes
+  int units;
 };
 template <int RM, int SPT>
 __device__ __forceinline__ bool tree_piece(TreeLine<RM, SPT>& line, int64_t u, int64_t u_end, TreePiece* x) {
   int64_t v = u, begin;
   x->kvh = 0;
-  if (v >= line.head_tiles) {
-    x->kvh = ((v | line.head_tiles) >> 32) == 0 ? (uint32_t)v / (uint32_t)line.head_tiles : (int)(v / line.head_tiles);
-    v -= x->kvh * line.head_tiles;
+  if (v >= line.head_units) {
+    x->kvh = ((v | line.head_units) >> 32) == 0 ? (uint32_t)v / (uint32_t)line.head_units : (int)(v / line.head_units);
+    v -= x->kvh * line.head_units;
   }
   if (line.find(v, &begin, &x->sq) < 0) return false;
   const int64_t in = v - begin;
-  x->span = (int)div64((uint64_t)in, (uint32_t)x->sq.tiles);
-  x->t0 = (int)(in - (int64_t)x->span * x->sq.tiles);
-  x->t1 = (int)min<int64_t>(x->sq.tiles, x->t0 + (u_end - u));
+  const int tiles = x->sq.tiles;
+  if (line.single) {
+    x->span = (int)div64((uint64_t)in, (uint32_t)x->sq.parts);
+    const int part = (int)(in - (int64_t)x->span * x->sq.parts);
+    const int each = ((uint32_t)tiles + (uint32_t)x->sq.parts - 1) / (uint32_t)x->sq.parts;
+    x->t0 = part * each;   // (no part is empty: fewer tiles each make no fewer parts)
+    x->t1 = min(tiles, x->t0 + each);
+    x->slot = 2 * (int)blockIdx.x;
+    x->units = 1;
+  } else {
+    x->span = (int)div64((uint64_t)in, (uint32_t)tiles);
+    x->t0 = (int)(in - (int64_t)x->span * tiles);
+    x->t1 = (int)min<int64_t>(tiles, x->t0 + (u_end - u));
+    // a share has at most one part that ends a span and one that begins one
+    x->slot = 2 * (int)blockIdx.x + (x->t0 == 0 ? 1 : 0);
+    x->units = x->t1 - x->t0;
+  }
   x->n_cached = x->sq.cached_subs();
   x->n_subs = x->n_cached + (line.p.k_new != nullptr ? (x->sq.n + SUB - 1) / SUB : 0);
-  x->whole = x->t0 == 0 && x->t1 == x->sq.tiles;
-  // a share has at most one part that ends a span and one that begins one
-  x->slot = 2 * (int)blockIdx.x + (x->t0 == 0 ? 1 : 0);
+  x->whole = x->t0 == 0 && x->t1 == tiles;
   return true;
 }
 
@@ -286,8 +344,8 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rl = lane & 31, hf = lane >> 5;   // row (N side) or key / channel (M side), half
   TreeLine<FEW_ROWS, FEW_WAVES> line(p);
-  int64_t u = blockIdx.x * line.share;
-  const int64_t u_end = min(line.head_tiles * p.n_kv_heads, u + line.share);
+  int64_t u, u_end;
+  line.mine_to_do(&u, &u_end);
   const int64_t tok_q = (int64_t)p.n_q_heads * D, tok_kv = (int64_t)p.n_kv_heads * D;
 
   while (u < u_end) {
@@ -595,7 +653,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
       }
       write(pc.span * FEW_ROWS + r, r, m, l, ch, o4);
     }
-    u += t1 - t0;
+    u += pc.units;
   }
 }
 
@@ -698,8 +756,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
       // (described anew for every piece: the lanes' sequences would take registers all along)
       TreeLine<MANY_ROWS, 2> line(p);
       if (first) {
-        u = blockIdx.x * line.share;
-        u_end = min(line.head_tiles * p.n_kv_heads, u + line.share);
+        line.mine_to_do(&u, &u_end);
         if (u >= u_end) return;
       }
       if (!tree_piece(line, u, u_end, &pc)) return;
@@ -1062,7 +1119,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
           else *(floatx4_t*)(part + ch) = x;
         }
     }
-    u += pc.t1 - pc.t0;
+    u += pc.units;
   }
 }
 
@@ -1085,13 +1142,17 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
   if (line.find_node(node, &before, &sq) < 0) return;   // behind the last tree
   const int row = (node - sq.q0) * p.group + (head - kvh * p.group);
   const int span = row / RM;
-  const int64_t a = kvh * line.head_tiles + before + (int64_t)span * sq.tiles;
-  const int w0 = (int)div64((uint64_t)a, (uint32_t)line.share);
-  const int n = (int)div64((uint64_t)(a + sq.tiles - 1), (uint32_t)line.share) - w0 + 1;
+  const int64_t a = kvh * line.head_units + before + (int64_t)span * (line.single ? sq.parts : sq.tiles);
+  int w0 = (int)a, n = sq.parts;
+  if (!line.single) {
+    w0 = (int)div64((uint64_t)a, (uint32_t)line.share);
+    n = (int)div64((uint64_t)(a + sq.tiles - 1), (uint32_t)line.share) - w0 + 1;
+  }
   if (n == 1) return;
-  // (the first part begins the span)
+  // (in a line cut anywhere the first part begins the span)
+  const int begins = line.single ? 0 : 1;
   auto at = [&](int k) __attribute__((always_inline)) {
-    return (int64_t)(2 * (w0 + k) + (k == 0 ? 1 : 0)) * RM + (row - span * RM);
+    return (int64_t)(2 * (w0 + k) + (k == 0 ? begins : 0)) * RM + (row - span * RM);
   };
   float m = -INFINITY, l = 0.f;
   vec_t o = {};
