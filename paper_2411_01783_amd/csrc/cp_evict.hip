@@ -520,8 +520,10 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Above this many slots a sequence, on average, they are cut into chunks.
-constexpr int64_t kChunkedSlots = 32768;
+// Above this many slots a sequence, on average, they are cut into chunks. us (a workgroup each, chunks), 4 sequences
+// of 8192 slots 19 and 41, 16384 29 and 42, 32768 48 and 42, 131072 231 and 43; 64 of 16384 43 and 57, of
+// 32768 63 and 60.
+constexpr int64_t kChunkedSlots = 28 * 1024;
 constexpr int kCachedKeys = 32768;   // keys in LDS at most: 128 KB
 
 struct EvictPlan {

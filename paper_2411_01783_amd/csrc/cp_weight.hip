@@ -96,16 +96,21 @@ struct RowAt {
   }
 };
 
-// KB: fragments of 32 keys that a wavefront holds. FLAT: one KV head, whose rows lie one behind the
+// A wavefront holds KB fragments of 32 keys: two of bf16 (one would halve the use of a row tile; us, one and two: 16
+// heads on one over 32 sequences of 2048 to 8192 keys, a query each 14.1 and 12.2, 16 queries each 28.3 and 24.5;
+// 32 heads on 8 over 8 sequences 63 and 28; 8192 queries over their own prompt 237 and 198; 16 queries over 8
+// times 4096 keys 11.4 and 13.2), one of fp32, of which two have no registers. FLAT: one KV head, whose rows lie one behind the
 // other in Q. A tile of 64 rows travels through registers into one of two LDS buffers while the
 // tile before it is used (16-byte chunk c of row r lies at c ^ (r % chunks): 16 lanes that read the same
 // chunk of neighbouring rows touch all banks).
 // Bound by the exponentials: a score costs a wavefront 24 clocks of vector issue (fma, exp at a quarter
 // of the rate, add) and 16 of the matrix pipe, so the products of a row and key block are issued
 // between the exponentials of the one before it.
-template <typename TI, int D, int KB, bool FLAT>
-__global__ __launch_bounds__(NW * 64, KB == 1 && sizeof(TI) == 2 ? 4 : 2) void kv_weight_kernel(
-    const WeightParams p) {
+template <typename TI>
+constexpr int frags() { return sizeof(TI) == 2 ? 2 : 1; }
+template <typename TI, int D, bool FLAT>
+__global__ __launch_bounds__(NW * 64, 2) void kv_weight_kernel(const WeightParams p) {
+  constexpr int KB = frags<TI>();
   constexpr int ROW = D * (int)sizeof(TI), CH = ROW / 16, NKS = CH / 2;
   constexpr int ST = TILE * CH / (NW * 64);        // chunks of a tile that a lane brings
   constexpr int RPI = NW * 64 / CH;                // rows that the workgroup brings at a time
@@ -395,19 +400,20 @@ __global__ __launch_bounds__(256) void kv_weight_sum_kernel(const WeightParams p
 }
 
 struct WeightPlan {
-  int kb;           // fragments of a wavefront
-  int64_t blocks;   // key blocks there can be
+  int wg_keys;      // keys of a block
+  int64_t blocks;   // there can be
   int n_ranges;
   size_t bytes;
 };
+// (what a workgroup's start costs, in tiles. us for 1, 3 and 5: 16 queries over 32 sequences 31.1, 24.4, 24.4; 64 over 2
+// of 8192 keys 14.3, 14.1, 18.3; 512 over 4 of 4096 55.2, 50.3, 50.3)
 constexpr double kStartTiles = 3;
 WeightPlan weight_plan(const cp_shape& s) {
   WeightPlan pl = {};
   const int64_t rows = (s.total_q * (s.n_q_heads / s.n_kv_heads) + s.batch - 1) / s.batch;
   const int64_t tiles = (rows + TILE - 1) / TILE;   // of a sequence, on average
-  pl.kb = tiles <= 1 || s.dtype == CP_FP32 ? 1 : 2;
-  const int wg_keys = NW * pl.kb * KEYS;
-  pl.blocks = s.total_kv / wg_keys + s.batch;
+  pl.wg_keys = NW * KEYS * (s.dtype == CP_FP32 ? frags<float>() : frags<bf16_t>());
+  pl.blocks = s.total_kv / pl.wg_keys + s.batch;
   // Ranges of the rows: as many as make the least of (rounds of workgroups, two a CU, and one for the
   // tail) times (tiles of one, and what it costs to begin). Which of them see nothing is not known here.
   int64_t n = 1;
@@ -468,25 +474,22 @@ extern "C" int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int
   p.total_q = s.total_q; p.total_kv = s.total_kv; p.batch = s.batch;
   p.n_q_heads = s.n_q_heads; p.n_kv_heads = s.n_kv_heads; p.group = s.n_q_heads / s.n_kv_heads;
   p.n_ranges = pl.n_ranges;
-  p.wg_keys = NW * pl.kb * KEYS;
+  p.wg_keys = pl.wg_keys;
   p.scale_log2 = (s.softmax_scale > 0.f ? s.softmax_scale : 1.0f / sqrtf((float)s.head_dim)) * kLog2e;
   p.decay = decay;
   hipStream_t st = (hipStream_t)stream;
   const dim3 grid((unsigned)pl.blocks, (unsigned)parts);
-#define CP_WEIGHT(TI, D, KB)                                                                        \
+#define CP_WEIGHT(TI, D)                                                                            \
   if (s.n_kv_heads == 1)                                                                            \
-    hipLaunchKernelGGL((kv_weight_kernel<TI, D, KB, true>), grid, dim3(NW * 64), 0, st, p);          \
+    hipLaunchKernelGGL((kv_weight_kernel<TI, D, true>), grid, dim3(NW * 64), 0, st, p);              \
   else                                                                                              \
-    hipLaunchKernelGGL((kv_weight_kernel<TI, D, KB, false>), grid, dim3(NW * 64), 0, st, p)
+    hipLaunchKernelGGL((kv_weight_kernel<TI, D, false>), grid, dim3(NW * 64), 0, st, p)
   if (s.dtype == CP_FP32) {
-    if (s.head_dim == 64) { CP_WEIGHT(float, 64, 1); }
-    else { CP_WEIGHT(float, 128, 1); }
-  } else if (s.head_dim == 64) {
-    if (pl.kb == 1) { CP_WEIGHT(bf16_t, 64, 1); }
-    else { CP_WEIGHT(bf16_t, 64, 2); }
+    if (s.head_dim == 64) { CP_WEIGHT(float, 64); }
+    else { CP_WEIGHT(float, 128); }
   } else {
-    if (pl.kb == 1) { CP_WEIGHT(bf16_t, 128, 1); }
-    else { CP_WEIGHT(bf16_t, 128, 2); }
+    if (s.head_dim == 64) { CP_WEIGHT(bf16_t, 64); }
+    else { CP_WEIGHT(bf16_t, 128); }
   }
 #undef CP_WEIGHT
   if (check_launch() != CP_OK) return CP_ERR_LAUNCH;
