@@ -59,7 +59,9 @@ __device__ __forceinline__ Range range_of(const int32_t* cu, int b, int64_t slot
 
 constexpr int SEL_THREADS = 1024, SEL_WAVES = SEL_THREADS / 64;
 constexpr int BINS = 2048;
-constexpr int CHUNK = 8192;               // slots of a chunk
+// Slots of a chunk. More chunks are read in fewer rounds but add more counts up: us for 8192, 4096 and 2048, 4 sequences of
+// 32768 slots 42, 34, 30, 16 of 65536 47, 39, 44, 64 of 32768 60, 64, 78.
+constexpr int CHUNK = 4096;
 constexpr int HIST = 3 * BINS + 64;       // three digits' counts, and the number of protected slots
 
 // Order-preserving key of a weight; protected slots are above all, NaN below all.
@@ -520,10 +522,10 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Above this many slots a sequence, on average, they are cut into chunks. us (a workgroup each, chunks), 4 sequences
-// of 8192 slots 19 and 41, 16384 29 and 42, 32768 48 and 42, 131072 231 and 43; 64 of 16384 43 and 57, of
-// 32768 63 and 60.
-constexpr int64_t kChunkedSlots = 28 * 1024;
+// Above this many slots a sequence, on average, they are cut into chunks. us (a workgroup each, chunks): 4 sequences
+// of 8192 slots 19 and 34, of 16384 29 and 34, of 32768 48 and 34, of 131072 232 and 35; 64 of 16384 43 and 50,
+// of 32768 63 and 64, of 65536 139 and 103.
+constexpr int64_t kChunkedSlots = 24 * 1024;
 constexpr int kCachedKeys = 32768;   // keys in LDS at most: 128 KB
 
 struct EvictPlan {
