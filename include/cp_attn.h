@@ -474,9 +474,9 @@ int cp_ring_prefill(const cp_ring_desc* desc, const cp_select_params* params, in
  *   kv_pos_cache      int32 [slots]
  *   cu_seqlens_kv     int32 [batch+1]: sequence b owns slots [cu[b], cu[b+1]), its capacity
  *   seq_used          int32 [batch+1]: tokens held per sequence (they fill the front of the
- *                     sequence's slot range in arrival order), followed by one word the
- *                     library uses as a ticket counter inside cp_kv_append; it is zero
- *                     between calls
+ *                     sequence's slot range, in arrival order until cp_kv_evict moves some),
+ *                     followed by one word the library uses as a ticket counter inside
+ *                     cp_kv_append; it is zero between calls
  * A slot that holds no token carries CP_POS_PAD_KV in kv_pos_cache, which no query position
  * reaches: cp_attn_decode, cp_attn_partial and the ring drivers take the cache (or one
  * sequence's slot range of it) as it is, with cu_seqlens_kv as the sequence boundaries.
@@ -558,6 +558,8 @@ int cp_tree_mask(int32_t batch, const int32_t* cu_seqlens, const int32_t* parent
  * are fp32; with bf16 inputs the probabilities are rounded to bf16 where out is bf16, and keep 24 bits
  * where it is fp32. Two launches. Boundaries and counts on the device that contradict the shape
  * are cut to it: nothing outside the tensors is read or written.
+ * Errors: as cp_attn_partial; CP_ERR_NULL also for one of k_new, v_new without the other, CP_ERR_SHAPE also
+ * for mask_words, and for total_q * n_q_heads or total_kv above INT32_MAX - 1024 or a batch above 2^24.
  */
 int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
                  const int32_t* cu_seqlens_q, const void* k_new, const void* v_new,
@@ -573,7 +575,9 @@ int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
  *   accepted  (device) int32 [batch]: the last accepted node, by its index within the tree; one
  *             that the tree does not have, or a negative one, accepts nothing
  *   dropped   (device) int32 or NULL: incremented by the number of rows that did not fit
- *   other arguments as cp_tree_attn and cp_kv_append. One launch, no workspace.
+ *   other arguments as cp_tree_attn and cp_kv_append. One launch, no workspace. k_new and v_new do
+ *   not overlap the cache; calls on one cache are ordered by the caller, as cp_kv_append's.
+ * Errors: as cp_kv_append, and CP_ERR_SHAPE for mask_words and for rows of more than 32 MB.
  */
 int cp_tree_accept(const cp_shape* shape, const void* k_new, const void* v_new,
                    const int32_t* pos_new, const int32_t* cu_seqlens_new, const uint64_t* tree_mask,
@@ -598,6 +602,8 @@ int cp_tree_accept(const cp_shape* shape, const void* k_new, const void* v_new,
  *   workspace cp_workspace_bytes(shape, CP_WS_WEIGHT) bytes, 256-byte aligned; may be NULL if 0
  * bf16 and fp32, head_dim 64 and 128, any group of query heads. fp32 arithmetic, sums in a fixed
  * order. What a query does not see does not reach the sum. One launch, or two with a workspace.
+ * Errors: as cp_attn_partial, and CP_ERR_SHAPE for a negative, infinite or NaN decay, total_kv above
+ * INT32_MAX - 256, total_q * n_q_heads above INT32_MAX - 64, or more than 65535 KV heads.
  */
 int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int32_t* q_pos,
                       const int32_t* cu_seqlens_q, const float* lse, const void* k_cache,
@@ -621,7 +627,10 @@ int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int32_t* q_pos
  *             which receives the kept tokens (what it held is given up; the source is left as it was); or
  *             all NULL and 0: in place. The two caches do not overlap.
  *   workspace cp_workspace_bytes(shape, CP_WS_EVICT) bytes, 256-byte aligned
- * Two launches. The result does not depend on the order in which anything runs.
+ * Two launches, or seven where the sequences have more than 24576 slots on average. The result does not
+ * depend on the order in which anything runs; calls on one cache are ordered by the caller.
+ * Errors: as cp_kv_append; CP_ERR_NULL for part of a destination, CP_ERR_SHAPE for sinks below 0, a batch above 65535,
+ * slots_to outside 0 .. INT32_MAX, or a destination that is the source; CP_ERR_WORKSPACE.
  */
 int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, int32_t* kv_pos_cache,
                 float* weight, const int32_t* cu_seqlens_kv, int32_t* seq_used,

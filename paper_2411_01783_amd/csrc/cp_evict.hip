@@ -479,6 +479,11 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_chunk_kernel(const EvictPar
   }
 }
 
+// (Where sequences' ranges overlap, against the layout, the lists of one may hold slots of another.)
+__device__ __forceinline__ int within(int slot, const Range& r) {
+  return (int)min((uint32_t)slot, (uint32_t)r.room - 1);   // (a range with rows has slots)
+}
+
 // Rows and bookkeeping: in place the moves, otherwise all slots that are filled, and those behind.
 __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
   const int b = blockIdx.y;
@@ -495,9 +500,11 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
       d = p.to[s0 + i];
     } else {
       const int m = p.to[s0 + i];
-      s = m >= 0 ? m : p.from[s0 - 1 - m];
+      s = m >= 0 ? m : p.from[s0 + within(-1 - m, from)];
       d = i;
     }
+    s = within(s, from);
+    d = within(d, to);
     const int64_t src = (s0 + s) * p.chunks + c, dst = (d0 + d) * p.chunks + c;
     const uint4 k = p.k[src], v = p.v[src];
     p.k_to[dst] = k;

@@ -399,6 +399,7 @@ __global__ __launch_bounds__(256) void kv_weight_sum_kernel(const WeightParams p
   }
 }
 
+constexpr int64_t kMaxParts = 65535;   // the grid's second dimension
 struct WeightPlan {
   int wg_keys;      // keys of a block
   int64_t blocks;   // there can be
@@ -418,7 +419,7 @@ WeightPlan weight_plan(const cp_shape& s) {
   // tail) times (tiles of one, and what it costs to begin). Which of them see nothing is not known here.
   int64_t n = 1;
   double least = 1e30;
-  for (int64_t i = 1; i <= 128 && i <= tiles; ++i) {
+  for (int64_t i = 1; i <= 128 && i <= tiles && i * s.n_kv_heads <= kMaxParts; ++i) {
     const double cost = ((double)(pl.blocks * s.n_kv_heads * i) / 512 + 1) *
                         (kStartTiles + (double)((tiles + i - 1) / i));
     if (cost < least) {
@@ -465,7 +466,7 @@ extern "C" int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int
                        workspace_bytes < pl.bytes))
     return CP_ERR_WORKSPACE;
   const int64_t parts = (int64_t)pl.n_ranges * s.n_kv_heads;
-  if (parts > 65535) return CP_ERR_SHAPE;   // the grid's second dimension
+  if (parts > kMaxParts) return CP_ERR_SHAPE;
   WeightParams p = {};
   p.q = q; p.q_pos = q_pos; p.cu_q = cu_seqlens_q;
   p.k = k_cache; p.kv_pos = kv_pos_cache; p.cu_kv = cu_seqlens_kv; p.used = seq_used;

@@ -675,3 +675,58 @@ def test_trees_of_many_rows_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_boundaries_that_contradict_the_shape_stay_inside(seed):
+    """Boundaries that fall, overlap or lie outside and counts beyond the room are cut to the tensors: what lies
+    around them stays as it was, and sequences that are described rightly get their results."""
+    rng = np.random.default_rng(seed)
+    nh, nkv, d, slots, t, guard = 16, 1, 128, 900, 40, 64
+    cu_kv = [0, 300, 600, 900] + list(rng.integers(-50, 1200, 3))
+    cu_q = [0, 10, 25, 40] + list(rng.integers(-20, 80, 3))
+    used = [250, 300, 17] + list(rng.integers(-5, 2000, 3)) + [0]
+    batch = len(cu_kv) - 1
+
+    def inside(shape, dtype, fill):
+        n = shape[0]
+        big = torch.full((n + 2 * guard,) + tuple(shape[1:]), fill, dtype=dtype, device="cuda")
+        return big, big[guard:guard + n]
+    cache = B.KVCache.__new__(B.KVCache)
+    cache.batch, cache.slots, cache.cu_host = batch, slots, np.asarray(cu_kv, dtype=np.int32)
+    cache.cu, cache.used, cache.dropped = i32(cu_kv), i32(used), i32([0])
+    (k_all, cache.k), (v_all, cache.v) = inside((slots, nkv, d), BF16, 3.0), inside((slots, nkv, d), BF16, 5.0)
+    pos_all, cache.kv_pos = inside((slots,), torch.int32, 11)
+    w_all, w = inside((slots,), F32, 2.0)
+    o_all, out = inside((t, nh, d), F32, 7.0)
+    l_all, lse = inside((t, nh), F32, 7.0)
+    k64, v64 = (np.round(rng.standard_normal((slots, nkv, d)) * 8) / 8 for _ in range(2))
+    cache.k.copy_(torch.as_tensor(k64))
+    cache.v.copy_(torch.as_tensor(v64))
+    kv_pos = np.concatenate([np.arange(300)] * 3).astype(np.int32)
+    cache.kv_pos.copy_(torch.as_tensor(kv_pos))
+    x = tree_inputs(171, [250, 300, 17], [10, 15, 15], nh, nkv, d, "bf16")
+    x["cu"] = np.asarray(cu_q, dtype=np.int32)
+    run_tree(cache, x, F32, out=out, lse=lse)
+    B.cp_kv_attn_weight(cache, dev(x["q"]), i32(x["q_pos"]), lse, w, i32(x["cu"]))
+    B.cp_tree_accept(cache, dev(x["k"]), dev(x["v"]), i32(x["q_pos"]), i32(x["cu"]), dev(x["mask"]),
+                     i32([9, 14, 14] + list(rng.integers(-3, 60, 3))))
+    into = B.KVCache([100] * batch, nkv, d)
+    into_w = torch.zeros(into.slots, device="cuda")
+    B.cp_kv_evict(cache, w, i32(rng.integers(-5, 500, batch)), into=into, into_weight=into_w)
+    B.cp_kv_evict(cache, w, i32(rng.integers(-5, 500, batch)))
+    torch.cuda.synchronize()
+    for big, fill in ((k_all, 3), (v_all, 5), (pos_all, 11), (w_all, 2), (o_all, 7), (l_all, 7)):
+        assert (big[:guard] == fill).all() and (big[-guard:] == fill).all()
+
+
+def test_boundaries_that_rise_beside_ones_that_do_not():
+    # the first sequences are right: what a later one claims does not change them
+    nh, nkv, d = 16, 1, 128
+    cache, host = make_cache(172, [250, 280], [300, 300], nkv, d)
+    x = tree_inputs(173, [250, 280], [10, 15], nh, nkv, d, "bf16")
+    want = run_tree(cache, x, F32)
+    cache.batch, cache.cu, cache.used = 3, i32([0, 300, 600, 900]), i32([250, 280, 40, 0])
+    x["cu"] = np.append(x["cu"], 70).astype(np.int32)
+    got = run_tree(cache, x, F32)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
