@@ -364,6 +364,35 @@ def test_attention_weight(name, decay):
     assert np.all(err <= tol[held] + 1e-30), (err / (tol[held] + 1e-30)).max()
 
 
+def test_calls_without_any_rows():
+    """No queries at all: the weights decay; no nodes: nothing happens; a cache without slots: the tree alone."""
+    cache, host = make_cache(53, [40, 7], [64, 9], 1, 128)
+    w0 = np.random.default_rng(3).random(cache.slots).astype(np.float32)
+    none = torch.empty((0, 16, 128), dtype=BF16, device="cuda")
+    for decay in (0.0, 0.5):
+        w = dev(w0.copy())
+        B.cp_kv_attn_weight(cache, none, i32([]), torch.empty((0, 16), device="cuda"), w, i32([0, 0, 0]), decay=decay)
+        want = w0.copy()
+        want[:40] *= decay
+        want[64:71] *= decay
+        assert np.array_equal(w.cpu().numpy(), want)
+    kv = torch.empty((0, 1, 128), dtype=BF16, device="cuda")
+    m = torch.empty((0, 1), dtype=torch.int64, device="cuda")
+    o, l = B.cp_tree_attn(cache, none, i32([]), kv, kv, i32([0, 0, 0]), m, out_dtype=F32)
+    assert o.shape == (0, 16, 128) and l.shape == (0, 16)
+    used = cache.used.tolist()
+    B.cp_tree_accept(cache, kv, kv, i32([]), i32([0, 0, 0]), m, i32([0, 0]))
+    assert cache.used.tolist() == used
+
+    empty = B.KVCache([0, 0], 1, 128)
+    x = tree_inputs(54, [0, 0], [40, 3], 16, 1, 128, "bf16")
+    host = dict(k=np.zeros((0, 1, 128)), v=np.zeros((0, 1, 128)), kv_pos=np.zeros(0, dtype=np.int32), used=[0, 0], cu=[0, 0, 0])
+    check_tree(run_tree(empty, x, F32), reference(x, host), 128, F32, False)
+    B.cp_tree_accept(empty, dev(x["k"]), dev(x["v"]), i32(x["q_pos"]), i32(x["cu"]), dev(x["mask"]), i32([5, 2]))
+    assert empty.used.tolist() == [0, 0, 0]
+    assert empty.dropped.item() == bits(x["mask"][[5]], 40).sum() + bits(x["mask"][[42]], 3).sum()
+
+
 def test_weights_of_finished_attention_sum_to_one():
     # with the LSE that the attention over the same keys returned, every row weighs 1 in all
     lens, nq, nh = [700, 130], [33, 130], 16
@@ -462,6 +491,17 @@ def test_evict(name, kind, protect):
             room = [max(1, b // 2) if i % 3 == 2 else max(b, 0) + 9 for i, b in enumerate(budget)]
             dst = make_cache(81, [min(2, r) for r in room], room, nkv, d, dtype)
         check_evict(cache, host, w, budget, keep_from, 4 if protect else 0, dst)
+
+
+@pytest.mark.parametrize("lens", [
+    [9500 if i % 100 == 7 else 3 + i % 60 for i in range(300)],    # more sequences than CUs, some beyond what LDS holds then
+    [25000 + 37 * i for i in range(67)],                           # in chunks, more than 64 sequences
+], ids=["many", "many_in_chunks"])
+def test_evict_many_sequences(lens):
+    budget = [n - n // 3 if i % 2 else n // 5 for i, n in enumerate(lens)]
+    rng = np.random.default_rng(4)
+    cache, host = make_cache(73, lens, [n + i % 3 for i, n in enumerate(lens)], 1, 8)
+    check_evict(cache, host, dev(weights_like(rng, cache.slots, "ties")), budget, [n - 2 for n in lens], 1)
 
 
 def test_evicting_again_changes_nothing():
