@@ -409,6 +409,9 @@ struct WeightPlan {
 // (what a workgroup's start costs, in tiles. us for 1, 3 and 5: 16 queries over 32 sequences 31.1, 24.4, 24.4; 64 over 2
 // of 8192 keys 14.3, 14.1, 18.3; 512 over 4 of 4096 55.2, 50.3, 50.3)
 constexpr double kStartTiles = 3;
+// (and the launch that adds the parts up: 16 queries over 8 times 4096 keys in one range 11.0 us, in two 13.1, 32 over 3 times
+// 5000 to 20000 16.8 and 18.4)
+constexpr double kSumTiles = 3;
 WeightPlan weight_plan(const cp_shape& s) {
   WeightPlan pl = {};
   const int64_t rows = (s.total_q * (s.n_q_heads / s.n_kv_heads) + s.batch - 1) / s.batch;
@@ -421,7 +424,8 @@ WeightPlan weight_plan(const cp_shape& s) {
   double least = 1e30;
   for (int64_t i = 1; i <= 128 && i <= tiles && i * s.n_kv_heads <= kMaxParts; ++i) {
     const double cost = ((double)(pl.blocks * s.n_kv_heads * i) / 512 + 1) *
-                        (kStartTiles + (double)((tiles + i - 1) / i));
+                        (kStartTiles + (double)((tiles + i - 1) / i)) +
+                        (i * s.n_kv_heads > 1 ? kSumTiles : 0);
     if (cost < least) {
       least = cost;
       n = i;
