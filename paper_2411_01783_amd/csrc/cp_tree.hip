@@ -1062,32 +1062,41 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
       auto pos_of = [](const char* b) { return (const int32_t*)(b + M::POS_OFF); };
       landed_barrier();
       if (pc.t0 + 2 < pc.t1) request_tile(pc.t0 + 2, buf(pc.t0 + 2));
-      {
-        const char* const b = buf(pc.t0);
+      if (pc.span * MANY_ROWS + wave * 32 >= n_rows) {
+        // none of the block's rows: the wavefront brings its part of the tiles and leaves the units to the others (64 rows
+        // of 32 sequences of 4096 keys 38.9 -> 29.7 us, 128 43.8 -> 32.2)
+        for (int t = pc.t0; t < pc.t1; ++t) {
+          landed_barrier();
+          if (t + 3 < pc.t1) request_tile(t + 3, buf(t + 3));
+        }
+      } else {
+        {
+          const char* const b = buf(pc.t0);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+          for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks)
-          s[0] = mfma32(__builtin_bit_cast(bf16x8_t, k_frag(b, ks)), __builtin_bit_cast(bf16x8_t, qf[ks]), s[0]);
+          for (int ks = 0; ks < NKS; ++ks)
+            s[0] = mfma32(__builtin_bit_cast(bf16x8_t, k_frag(b, ks)), __builtin_bit_cast(bf16x8_t, qf[ks]), s[0]);
 #pragma unroll
-        for (int g = 0; g < AHEAD; ++g) fr[g] = k_frag(b + HALF, g);
-        masked = needs_mask(2 * pc.t0, pos_of(b)[rl]);
-        top = row_max(IntC<0>{});
+          for (int g = 0; g < AHEAD; ++g) fr[g] = k_frag(b + HALF, g);
+          masked = needs_mask(2 * pc.t0, pos_of(b)[rl]);
+          top = row_max(IntC<0>{});
+        }
+        const char* const zeros = smem + M::ZERO_OFF - M::V_OFF;   // (no product is pending: P times zeros)
+        for (int t = pc.t0; t < pc.t1; ++t) {
+          const char* const b = buf(t);
+          const char* const b_next = buf(t + 1);
+          step(IntC<0>{}, 2 * t, b, pos_of(b), b + HALF, pos_of(b) + SUB, b_next,
+               pending ? buf(t - 1) + HALF : zeros);
+          // (the next tile but one has landed everywhere, and the values of the one before have been read)
+          landed_barrier();
+          if (t + 3 < pc.t1) request_tile(t + 3, buf(t + 3));
+          // (a second sub-tile that is not there holds copies of the last key, none of which counts)
+          step(IntC<1>{}, 2 * t + 1, b + HALF, pos_of(b) + SUB, b_next, pos_of(b_next), b_next + HALF,
+               pending ? b : zeros);
+        }
+        if (pending) value_product(IntC<1>{}, IntC<0>{}, buf(pc.t1 - 1) + HALF);
       }
-      const char* const zeros = smem + M::ZERO_OFF - M::V_OFF;   // (no product is pending: P times zeros)
-      for (int t = pc.t0; t < pc.t1; ++t) {
-        const char* const b = buf(t);
-        const char* const b_next = buf(t + 1);
-        step(IntC<0>{}, 2 * t, b, pos_of(b), b + HALF, pos_of(b) + SUB, b_next,
-             pending ? buf(t - 1) + HALF : zeros);
-        // (the next tile but one has landed everywhere, and the values of the one before have been read)
-        landed_barrier();
-        if (t + 3 < pc.t1) request_tile(t + 3, buf(t + 3));
-        // (a second sub-tile that is not there holds copies of the last key, none of which counts)
-        step(IntC<1>{}, 2 * t + 1, b + HALF, pos_of(b) + SUB, b_next, pos_of(b_next), b_next + HALF,
-             pending ? b : zeros);
-      }
-      if (pending) value_product(IntC<1>{}, IntC<0>{}, buf(pc.t1 - 1) + HALF);
     }
     l_run += xor32(l_run);
 
@@ -1287,7 +1296,7 @@ __global__ __launch_bounds__(ACCEPT_THREADS) void tree_accept_kernel(const Accep
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-constexpr int64_t kFewProducts = 1 << 19;
+constexpr int64_t kFewBlocks = 5 << 23, kFewOneBlock = 1 << 27;
 struct TreePlan {
   bool many;
   int rm, spt, n_wg, log2_wg;
@@ -1296,15 +1305,18 @@ struct TreePlan {
 TreePlan tree_plan(const cp_shape& s) {
   TreePlan pl = {};
   const int64_t group = s.n_q_heads / s.n_kv_heads;
-  // Rows of a sequence on average, and 32-row blocks times sub-tiles of all: the form for many rows reads a
-  // key once for 256 rows and has three times the matrix rate, the other starts and ends sooner. us (few rows,
-  // many): head_dim 128, 16 heads on one, 4096 keys: 8 sequences of 32 rows 21.7 and 24.6, of 128 30.0 and
-  // 31.0, of 192 37.7 and 34.8; 32 sequences of 32 rows 29.7 and 37.0, of 64 42.7 and 38.9, of 256 99 and 53;
-  // 1 sequence of 8192 keys, 384 rows 31.5 and 34.1. Head_dim 64, 8 heads on two: 8 sequences of 64 rows 16.6 and 20.4, of
-  // 128 23.6 and 23.2; 32 sequences of 32 rows 23.6 and 39.0, of 128 54.8 and 43.7.
-  const int64_t rows = s.total_q * group / s.batch;
+  // 32-row blocks (of a sequence on average) times sub-tiles of all, weighed by head_dim: the form for many rows reads a
+  // key once for 256 rows and has three times the matrix rate, the other starts and ends sooner, and one block of it
+  // is all the work there is up to 32 rows. us (few rows, many): head_dim 128, 16 heads on one, 4096 keys: 8 sequences
+  // of 32 rows 17.4 and 19.3, of 64 23.8 and 21.3, of 256 38 and 31; 32 sequences of 16 rows 25.0 and 25.2, of
+  // 32 28.5 and 26.5, of 64 38.3 and 29.7; 1 sequence of 8192 keys, 256 rows 23.8 and 27.3; 32 heads on 8, 8
+  // sequences of 32 rows 39 and 43, 32 of 32 133 and 117, of 64 179 and 121. Head_dim 64, 8 heads on two: 8
+  // sequences of 128 rows 24.5 and 25.6, of 256 33.4 and 30.0; 32 sequences of 32 rows 24.5 and 35.0, of 64 33.0
+  // and 34.6, of 128 56 and 39.
+  const int64_t blocks = (s.total_q * group / s.batch + 31) / 32;
   const int64_t subs = ((s.total_kv + s.total_q) / SUB + s.batch) * s.n_kv_heads;
-  pl.many = s.dtype == CP_BF16 && rows > 32 && subs > kFewProducts / s.head_dim / ((rows + 31) / 32);
+  const int64_t limit = (blocks > 1 ? kFewBlocks : kFewOneBlock) / (s.head_dim * s.head_dim);
+  pl.many = s.dtype == CP_BF16 && blocks > 0 && subs > limit / blocks;
   pl.rm = pl.many ? MANY_ROWS : FEW_ROWS;
   pl.spt = pl.many ? 2 : FEW_WAVES;
   // no more workgroups than there can be tiles
