@@ -61,6 +61,7 @@ struct TreeParams {
 struct TreeSeq {
   int32_t q0, n, k0, used;   // first node, nodes, first cache slot, tokens in the cache
   int32_t spans, tiles;      // row blocks of a KV head, tiles of each
+  int32_t rm;                // rows of a row block: a multiple of 32, much the same for all of them
   int32_t parts;             // of each, where every workgroup takes one
   __device__ __forceinline__ TreeSeq of_lane(int l) const {
     TreeSeq r;
@@ -70,6 +71,7 @@ struct TreeSeq {
     r.used = __builtin_amdgcn_readlane(used, l);
     r.spans = __builtin_amdgcn_readlane(spans, l);
     r.tiles = __builtin_amdgcn_readlane(tiles, l);
+    r.rm = __builtin_amdgcn_readlane(rm, l);
     r.parts = __builtin_amdgcn_readlane(parts, l);
     return r;
   }
@@ -116,7 +118,12 @@ struct TreeLine {
     mine.n = (int32_t)clamp64(a1, mine.q0, p.total_q) - mine.q0;
     mine.k0 = (int32_t)clamp64(c0, 0, p.total_kv);
     mine.used = (int32_t)clamp64(u, 0, clamp64(c1, mine.k0, p.total_kv) - mine.k0);
-    mine.spans = (mine.n * p.group + RM - 1) / RM;   // (rows of a KV head in 31 bits: the host checks)
+    const int rows = mine.n * p.group;               // (in 31 bits: the host checks)
+    mine.spans = (rows + RM - 1) / RM;
+    // (blocks of the same height: the longest share decides. us, full blocks and a rest against equal ones: 272 rows on
+    // 8192 keys 26.0 and 23.7, on 8 times 4096 of 8 KV heads 103 and 90, 384 rows 107.5 and 98.2, 640 150 and 153)
+    const uint32_t groups = (uint32_t)(rows + 31) / 32, spans = (uint32_t)max(mine.spans, 1);
+    mine.rm = RM == 32 ? 32 : (int)((groups + spans - 1) / spans) * 32;
     if (b0 + (int)(threadIdx.x & 63) >= p.batch) mine.spans = 0;
     const int subs = mine.cached_subs() + (p.k_new != nullptr ? (mine.n + SUB - 1) / SUB : 0);
     mine.tiles = subs > 0 ? (subs + SPT - 1) / SPT : 1;   // (nothing to see: one tile, empty)
@@ -764,8 +771,9 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
     const TreeSeq& sq = pc.sq;
     const int kvh = pc.kvh, n_cached = pc.n_cached, n_subs = pc.n_subs;
     const int n_rows = sq.n * p.group;
-    const int row = pc.span * MANY_ROWS + wave * 32 + rl;
-    const bool ok = row < n_rows;
+    const int row = pc.span * sq.rm + wave * 32 + rl;
+    const bool busy = wave * 32 < sq.rm && pc.span * sq.rm + wave * 32 < n_rows;
+    const bool ok = busy && row < n_rows;
     const int nd = ok ? (uint32_t)row / (uint32_t)p.group : 0;
     const int node = sq.q0 + nd;
     const int head = kvh * p.group + (ok ? row - nd * p.group : 0);
@@ -1062,7 +1070,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
       auto pos_of = [](const char* b) { return (const int32_t*)(b + M::POS_OFF); };
       landed_barrier();
       if (pc.t0 + 2 < pc.t1) request_tile(pc.t0 + 2, buf(pc.t0 + 2));
-      if (pc.span * MANY_ROWS + wave * 32 >= n_rows) {
+      if (!busy) {
         // none of the block's rows: the wavefront brings its part of the tiles and leaves the units to the others (64 rows
         // of 32 sequences of 4096 keys 38.9 -> 29.7 us, 128 43.8 -> 32.2)
         for (int t = pc.t0; t < pc.t1; ++t) {
@@ -1150,7 +1158,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
   int64_t before;
   if (line.find_node(node, &before, &sq) < 0) return;   // behind the last tree
   const int row = (node - sq.q0) * p.group + (head - kvh * p.group);
-  const int span = row / RM;
+  const int span = (uint32_t)row / (uint32_t)sq.rm;
   const int64_t a = kvh * line.head_units + before + (int64_t)span * (line.single ? sq.parts : sq.tiles);
   int w0 = (int)a, n = sq.parts;
   if (!line.single) {
@@ -1161,7 +1169,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
   // (in a line cut anywhere the first part begins the span)
   const int begins = line.single ? 0 : 1;
   auto at = [&](int k) __attribute__((always_inline)) {
-    return (int64_t)(2 * (w0 + k) + (k == 0 ? begins : 0)) * RM + (row - span * RM);
+    return (int64_t)(2 * (w0 + k) + (k == 0 ? begins : 0)) * RM + (row - span * sq.rm);
   };
   float m = -INFINITY, l = 0.f;
   vec_t o = {};
