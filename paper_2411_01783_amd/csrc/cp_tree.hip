@@ -144,7 +144,7 @@ struct TreeLine {
     }
     const int64_t all = head_units * p.n_kv_heads;
     share = (all + p.n_wg - 1) >> p.log2_wg;
-    if (share == 1) return;   // (no share has two pieces)
+    if (share <= 1) return;   // (no share has two pieces)
     int64_t spans = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 64) {
       if (b0 != held) hold(b0);

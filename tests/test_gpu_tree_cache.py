@@ -386,6 +386,12 @@ def test_calls_without_any_rows():
     B.cp_tree_accept(cache, kv, kv, i32([]), i32([0, 0, 0]), m, i32([0, 0]))
     assert cache.used.tolist() == used
 
+    x = tree_inputs(55, [40, 7], [3, 2], 16, 1, 128, "bf16")   # rows, but of no tree
+    x["cu"] = ends([0, 0])
+    out, lse = torch.full((5, 16, 128), 7.0, device="cuda"), torch.full((5, 16), 7.0, device="cuda")
+    run_tree(cache, x, F32, out=out, lse=lse)
+    assert (out == 7).all() and (lse == 7).all()
+
     empty = B.KVCache([0, 0], 1, 128)
     x = tree_inputs(54, [0, 0], [40, 3], 16, 1, 128, "bf16")
     host = dict(k=np.zeros((0, 1, 128)), v=np.zeros((0, 1, 128)), kv_pos=np.zeros(0, dtype=np.int32), used=[0, 0], cu=[0, 0, 0])
