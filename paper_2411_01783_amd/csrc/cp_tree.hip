@@ -338,7 +338,7 @@ constexpr int few_smem() {
 
 // Bound by latencies: the chain {sequence boundaries} -> K, V, Q -> products -> join in LDS -> parts, and the
 // second launch; 8 nodes of 16 heads over 430 keys take 9 us here and 4 in the join, 32 sequences of 4096 keys at
-// 32 rows each 29.7 us (67 MB, 2.3 TB/s).
+// 32 rows each 28.5 us (67 MB, 2.4 TB/s).
 // TI: K, V and Q. TO: O. P goes into the second product as TERMS bf16 terms (bf16 inputs): one
 // where O is rounded to bf16 itself, three (24 bits) where it stays fp32.
 template <typename TI, int D, int TERMS, typename TO>
@@ -670,15 +670,16 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
 // A step works on three sub-tiles: the products S^T of the next one and O^T of the one before are issued
 // between the softmax arithmetic of the current one, which needs neither, and so is the maximum of the
 // next one's scores. The reference that the exponentials are taken against is raised only when a
-// score exceeds it by 2^8 (O and the sum are rescaled then): it cancels in O / l, and what is rounded
-// has the same relative error at any scale.
+// score exceeds it by 8 in powers of two (O and the sum are rescaled then): it cancels in O / l, and what is
+// rounded has the same relative error at any scale.
 // A tile goes straight into one of four LDS buffers: the tile before (its values), the current one, the next
 // and the one being filled; one barrier a tile. (Through registers, with fragments requested four products ahead
 // where now eight fit: 97 and 104 us for 61 nodes of 16 heads over 131072 keys, 88 and 95 for 16 sequences of 2048
 // to 8192 keys with three terms.)
-// Measured: 61 nodes of 16 heads over 131072 keys of one, 94 us, 700 TFLOP/s, of which 75 us are the loop (2050 cycles of
-// a tile's 3900 the matrix pipe), 11 the way to the first product and 5 the parts' way out. No one unit binds the loop:
-// without its LDS reads the call takes 0.92 of the time, without the exponentials 0.98, without the loads 0.92.
+// Measured: 61 nodes of 16 heads over 131072 keys of one, 85 us, 770 TFLOP/s, of which 70 us are the loop (the matrix
+// pipe takes 2050 cycles of a tile's 3600), 9 the way to the first product and 4 the parts' way out. No one unit binds
+// the loop: without its LDS reads the call takes 0.92 of the time, without the exponentials 0.98, without the loads
+// 0.92; first requests by turns of the two wavefronts of a SIMD (their priority) change nothing.
 // ---------------------------------------------------------------------------
 constexpr int MANY_WAVES = 8;
 constexpr int MANY_ROWS = 32 * MANY_WAVES;
