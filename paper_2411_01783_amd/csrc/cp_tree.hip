@@ -1305,7 +1305,7 @@ __global__ __launch_bounds__(ACCEPT_THREADS) void tree_accept_kernel(const Accep
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-constexpr int64_t kFewBlocks = 5 << 23, kFewOneBlock = 1 << 27;
+constexpr int64_t kFewBlocks = 1 << 26, kFewOneBlock = 1 << 27, kFewTiles = 768;
 struct TreePlan {
   bool many;
   int rm, spt, n_wg, log2_wg;
@@ -1316,12 +1316,12 @@ TreePlan tree_plan(const cp_shape& s) {
   const int64_t group = s.n_q_heads / s.n_kv_heads;
   // 32-row blocks (of a sequence on average) times sub-tiles of all, weighed by head_dim: the form for many rows reads a
   // key once for 256 rows and has three times the matrix rate, the other starts and ends sooner, and one block of it
-  // is all the work there is up to 32 rows. us (few rows, many): head_dim 128, 16 heads on one, 4096 keys: 8 sequences
-  // of 32 rows 17.4 and 19.3, of 64 23.8 and 21.3, of 256 38 and 31; 32 sequences of 16 rows 25.0 and 25.2, of
-  // 32 28.5 and 26.5, of 64 38.3 and 29.7; 1 sequence of 8192 keys, 256 rows 23.8 and 27.3; 32 heads on 8, 8
-  // sequences of 32 rows 39 and 43, 32 of 32 133 and 117, of 64 179 and 121. Head_dim 64, 8 heads on two: 8
-  // sequences of 128 rows 24.5 and 25.6, of 256 33.4 and 30.0; 32 sequences of 32 rows 24.5 and 35.0, of 64 33.0
-  // and 34.6, of 128 56 and 39.
+  // is all the work there is up to 32 rows. us (few rows, many): head_dim 128, 16 heads on one: 8 sequences of 4096
+  // keys, 32 rows 17.5 and 19.5, 128 29.2 and 25.9, 256 39 and 32; 1 of 8192 keys, 256 rows 18.8 and 27.6, 640
+  // 26.4 and 29.9; 1 of 16384, 256 rows 28.2 and 30.5, 640 33.7 and 32.1; 32 sequences of 16 rows 25.0 and 25.2, of 64 38.3
+  // and 29.7; 32 heads on 8, 8 sequences of 32 rows 39 and 43, 32 of 32 133 and 117, of 64 179 and 121. Head_dim 64,
+  // 8 heads on two: 8 sequences of 128 rows 24.5 and 25.6, of 256 33.4 and 30.0; 32 sequences of 32 rows 24.5 and
+  // 35.0, of 64 33.0 and 34.6, of 128 56 and 39.
   const int64_t blocks = (s.total_q * group / s.batch + 31) / 32;
   const int64_t subs = ((s.total_kv + s.total_q) / SUB + s.batch) * s.n_kv_heads;
   const int64_t limit = (blocks > 1 ? kFewBlocks : kFewOneBlock) / (s.head_dim * s.head_dim);
@@ -1331,7 +1331,10 @@ TreePlan tree_plan(const cp_shape& s) {
   // no more workgroups than there can be tiles
   const int64_t spans = s.total_q * group / pl.rm + s.batch;
   const int64_t tiles = (s.total_kv + s.total_q) / (SUB * pl.spt) + 2 * (int64_t)s.batch;
-  const int64_t most = pl.many ? 256 : 512;
+  // (two workgroups of the form for few rows share a CU, which pays from a few tiles each. us for 256 and 512: 1 sequence
+  // of 8192 keys, 256 rows 18.8 and 23.8, 640 rows 28.2 and 26.4; 8 of 1024, 128 rows 18.0 and 20.6, 8 of 4096, 256
+  // rows 45 and 39; 32 heads on 8, 2048 keys, 64 rows 17.1 and 19.1)
+  const int64_t most = pl.many || blocks * subs / FEW_WAVES <= kFewTiles ? 256 : 512;
   const int64_t any = spans > most || tiles > most ? most : spans * tiles * s.n_kv_heads;
   while ((1 << pl.log2_wg) < any && (1 << pl.log2_wg) < most) ++pl.log2_wg;
   pl.n_wg = 1 << pl.log2_wg;

@@ -63,9 +63,10 @@ TREES = {
                8, 2, 128, "bf16"),
     "m_odd_group": ([2500, 31], [131, 130], 15, 3, 128, "bf16"),
     "m_one_more": ([16417], [257], 2, 2, 128, "bf16"),
-    "m_d64": ([3303, 700], [100, 61], 32, 2, 64, "bf16"),
+    "d64_mid": ([3303, 700], [100, 61], 32, 2, 64, "bf16"),
+    "m_d64": ([7003, 700], [100, 61], 32, 2, 64, "bf16"),
     "d64_seqs": ([500 + 131 * (i % 7) for i in range(70)], [9 + i % 8 for i in range(70)], 8, 2, 64, "bf16"),
-    "m_d64_seqs": ([900 + 131 * (i % 7) for i in range(70)], [9 + i % 8 for i in range(70)], 8, 2, 64, "bf16"),
+    "m_d64_seqs": ([1500 + 131 * (i % 7) for i in range(70)], [9 + i % 8 for i in range(70)], 8, 2, 64, "bf16"),
     "m_few_rows": ([26000, 9001], [3, 4], 16, 8, 128, "bf16"),
     "fp32": ([200, 0, 333], [5, 33, 66], 4, 1, 64, "fp32"),
     "fp32_128": ([200, 129], [9, 2], 6, 2, 128, "fp32"),
