@@ -700,9 +700,11 @@ __device__ __forceinline__ float halves_max(float x) {
 // Requests from memory into LDS, 16 or 4 bytes a lane at `dst` (uniform) and on. In assembly: in front of
 // every LDS read the compiler would wait for the requests that it knows of. landed_barrier() waits for them.
 // (No vector register is written. m0 is the compiler's own: it holds nothing across statements, each use sets
-// it. The s_nop is the wait state between its write and its use.)
+// it. The s_nop 0 is the wait state between its write and its use. A base in scalar registers may have been written
+// by the vector instruction in front of the statement, a v_readlane that brings a spilled one back: a memory instruction
+// may read it 5 wait states later, which the compiler keeps for instructions of its own alone.)
 __device__ __forceinline__ void dma16(const void* base, uint32_t lane_bytes, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %1"
                :: "v"(lane_bytes), "s"(base), "s"(dst) : "memory");
 }
 __device__ __forceinline__ void dma16(const void* src, uint32_t dst) {
