@@ -322,9 +322,34 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t x) {
   if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
   return x;
 }
-__device__ __forceinline__ uint32_t any_not_finite(uint32_t x) {   // 1 or 0, without a branch
-  return (uint32_t)((x & 0x7f80u) == 0x7f80u) | (uint32_t)((x & 0x7f800000u) == 0x7f800000u);
+// bf16 pair: 1.0 where bit i (low half), bit i + 1 (high half) of `bits` is set.
+__device__ __forceinline__ uint32_t ones_of(uint32_t bits, int i) {
+  return ((bits >> i) & 1u ? 0x3f80u : 0) | ((bits >> (i + 1)) & 1u ? 0x3f800000u : 0);
 }
+
+// V that is not finite. A row that does not see it must not meet it (its weight is 0, and 0 times it is a NaN), and
+// one that sees an infinity has it as its result, whatever the weight (which may have become 0, and whose second and third
+// term may be negative: a NaN again). What the plain product leaves in such a row is the right infinity or a NaN, never
+// a finite number or the wrong sign. So nothing looks for such values on the way; where a result holds a NaN, the piece is
+// gone through a second time, with the values that are not finite set apart from the others in every sub-tile.
+// NaN if the blocks hold one (or maybe an infinity: then the second pass is in vain).
+template <int N>
+__device__ __forceinline__ float nan_of(const floatx16_t (&o)[N]) {
+  float x = 0.f;
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) x = fmaf(o[b][i], o[b][i + 1], x);
+  return x;
+}
+// x * f of the second pass: an infinity that has been seen stays, however small the factor.
+__device__ __forceinline__ float scaled(float x, float f) {
+  return fabsf(x) == INFINITY ? x : x * f;
+}
+template <int J>
+struct IntC {
+  static constexpr int value = J;
+};
 
 // Few rows: the four wavefronts of a workgroup hold the same 32 rows and take turns at the sub-tiles (the keys
 // are what there is to share out), each with a buffer of its own; a tile is a sub-tile for each of them.
@@ -412,19 +437,36 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
       q_max = max(q_max, __shfl_xor(q_max, o, 64));
     }
 
-    float m_run = -INFINITY, l_run = 0.f;
+    float m_run, l_run;
     floatx16_t o_acc[NCB];
+    // f(i, whether the lane's row sees the key of score i) for sub-tile st of `cnt` keys; score i of lane
+    // (rl, hf): key (i / 4) * 8 + hf * 4 + i % 4
+    auto each_score = [&](int st, bool own, int cnt, auto f) __attribute__((always_inline)) {
+      const uint32_t there = cnt == SUB ? ~0u : (1u << cnt) - 1;
+      uint32_t see = there;
+      if (own) {
+        const int word = (st - n_cached) >> 1;
+        see = 0;
+        if (ok && word < p.words)
+          see = (uint32_t)(p.mask[(int64_t)node * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
+      }
+      see >>= hf * 4;   // (bit a * 8 + i: score 4 a + i)
 #pragma unroll
-    for (int cb = 0; cb < NCB; ++cb)
+      for (int a = 0; a < 4; ++a) {
+        const int4 x = *(const int4*)(buf + T::POS_OFF + (a * 8 + hf * 4) * 4);
+        const int32_t kp[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o_acc[cb][i] = 0.f;
-
-    // S, P and O of one sub-tile that lies in LDS at `buf`.
-    auto compute = [&](int st) __attribute__((always_inline)) {
+        for (int i = 0; i < 4; ++i)
+          f(4 * a + i, ((int)((see & (1u << (a * 8 + i))) != 0) & ((int)own | (int)(kp[i] <= qp))) != 0);
+      }
+    };
+    // S, P and O of one sub-tile that lies in LDS at `buf`. AGAIN: of the second pass.
+    auto compute = [&](auto againc, int st) __attribute__((always_inline)) {
+      constexpr bool AGAIN = decltype(againc)::value != 0;
       const bool own = st >= n_cached;
       const int first = (own ? st - n_cached : st) * SUB;
       const int cnt = min(SUB, (own ? sq.n : sq.used) - first);
-      bool masked = own || cnt < SUB;
+      bool masked = AGAIN || own || cnt < SUB;
       if (!own) {
         const int32_t kp = *(const int32_t*)(buf + T::POS_OFF + rl * 4);
         if (__builtin_amdgcn_ballot_w64(kp <= q_max) == 0) return;   // none of the rows sees any
@@ -445,40 +487,12 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
           s = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, qf[ks]), s);
         }
       }
-      // score i of lane (rl, hf): key (i / 4) * 8 + hf * 4 + i % 4
-      bool odd_v = false;   // V holds what is not finite, which rows that do not see it must not meet
-      if (masked) {
-        const uint32_t there = cnt == SUB ? ~0u : (1u << cnt) - 1;
-        uint32_t see = there;
-        if (own) {
-          const int word = (st - n_cached) >> 1;
-          see = 0;
-          if (ok && word < p.words)
-            see = (uint32_t)(p.mask[(int64_t)node * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
-        }
-        see >>= hf * 4;   // (bit a * 8 + i: score 4 a + i)
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-          const int4 x = *(const int4*)(buf + T::POS_OFF + (a * 8 + hf * 4) * 4);
-          const int32_t kp[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int vis = (int)((see & (1u << (a * 8 + i))) != 0) & ((int)own | (int)(kp[i] <= qp));
-            s[4 * a + i] = vis != 0 ? s[4 * a + i] : -INFINITY;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < SUB * T::ROW / 1024; ++i) {
-          const uint4 x = *(const uint4*)(buf + T::V_OFF + i * 1024 + lane * 16);
-          if constexpr (F32)
-            odd_v |= (x.x & 0x7f800000u) == 0x7f800000u || (x.y & 0x7f800000u) == 0x7f800000u ||
-                     (x.z & 0x7f800000u) == 0x7f800000u || (x.w & 0x7f800000u) == 0x7f800000u;
-          else
-            odd_v |= (any_not_finite(x.x) | any_not_finite(x.y) | any_not_finite(x.z) |
-                      any_not_finite(x.w)) != 0;
-        }
-        odd_v = __builtin_amdgcn_ballot_w64(odd_v) != 0;
-      }
+      uint32_t seen_bits = 0;   // of the second pass: bit i, the row sees the key of score i
+      if (masked)
+        each_score(st, own, cnt, [&](int i, bool vis) {
+          s[i] = vis ? s[i] : -INFINITY;
+          if (AGAIN) seen_bits |= (uint32_t)vis << i;
+        });
       u32x4_t pb[TERMS][2];   // P^T of keys 0..15 and 16..31, per term
       float e[16];
       float mx = s[0];
@@ -508,7 +522,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
 #pragma unroll
         for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) o_acc[cb][i] *= alpha;
+          for (int i = 0; i < 16; ++i) o_acc[cb][i] = AGAIN ? scaled(o_acc[cb][i], alpha) : o_acc[cb][i] * alpha;
       }
       if constexpr (F32) {
         // O^T += V^T P^T, a key pair a step: k slot hf of step i is the key of score i
@@ -521,17 +535,17 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
           for (int i = 0; i < 16; ++i) {
             const int r = (i >> 2) * 8 + hf * 4 + (i & 3);
             float v = *(const float*)(buf + T::V_OFF + r * T::ROW + (cb * 32 + rl) * 4);
-            if (odd_v) {
+            if constexpr (AGAIN) {
               const bool fin = fabsf(v) < INFINITY;
               const float up = fin || v == -INFINITY ? 0.f : 1.f, dn = fin || v == INFINITY ? 0.f : 1.f;
-              const float seen = e[i] != 0.f ? 1.f : 0.f;
+              const float seen = (seen_bits >> i) & 1u ? 1.f : 0.f;
               plus = mfma32(up, seen, plus);
               minus = mfma32(dn, seen, minus);
               v = fin ? v : 0.f;
             }
             o_acc[cb] = mfma32(v, e[i], o_acc[cb]);
           }
-          if (odd_v) {
+          if constexpr (AGAIN) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               o_acc[cb][i] += (plus[i] > 0.f ? INFINITY : 0.f) + (minus[i] > 0.f ? -INFINITY : 0.f);
@@ -555,7 +569,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
               v[kb][2 * x] = z[0];
               v[kb][2 * x + 1] = z[1];
             }
-          if (__builtin_expect(odd_v, 0)) {
+          if constexpr (AGAIN) {
             floatx16_t sign[2];   // how many visible infinities of either sign (a NaN: both)
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
@@ -567,8 +581,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                   a[x] = not_finite(v[kb][x], m == 1);
-                  seen[x] = ((pb[0][kb][x] & 0xffffu) != 0 ? 0x3f80u : 0) |
-                            ((pb[0][kb][x] >> 16) != 0 ? 0x3f800000u : 0);
+                  seen[x] = ones_of(seen_bits, kb * 8 + 2 * x);
                 }
                 sign[m] = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, seen), sign[m]);
               }
@@ -591,15 +604,30 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
       }
     };
 
-    for (int t = t0; t < t1; ++t) {   // (a wavefront waits for its own sub-tiles alone)
-      const int st = t * FEW_WAVES + wave;
-      if (st >= n_subs) break;
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      compute(st);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (t + 1 < t1 && st + FEW_WAVES < n_subs) request(st + FEW_WAVES);
+    auto pass = [&](auto againc) __attribute__((always_inline)) {
+      m_run = -INFINITY;
+      l_run = 0.f;
+#pragma unroll
+      for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o_acc[cb][i] = 0.f;
+      for (int t = t0; t < t1; ++t) {   // (a wavefront waits for its own sub-tiles alone)
+        const int st = t * FEW_WAVES + wave;
+        if (st >= n_subs) break;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        compute(againc, st);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (t + 1 < t1 && st + FEW_WAVES < n_subs) request(st + FEW_WAVES);
+      }
+      l_run += xor32(l_run);
+    };
+    pass(IntC<0>{});
+    const float x = nan_of<NCB>(o_acc);
+    // (a row whose sum is a NaN is NaN in any case; without a sub-tile O is 0)
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(ok && l_run == l_run && x != x) != 0, 0)) {
+      request(t0 * FEW_WAVES + wave);
+      pass(IntC<1>{});
     }
-    l_run += xor32(l_run);
 
     // ---- the span's result, or this share's part of it ----
     auto write = [&](int r, int in_block, float m, float l, int ch, floatx4_t o4) {
@@ -642,7 +670,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
       const int r = i * RPI + tid / LPR, ch = (tid % LPR) * 4;
       float m = -INFINITY, l = 0.f;
       floatx4_t o4 = {0.f, 0.f, 0.f, 0.f};
-      float mw[FEW_WAVES], lw[FEW_WAVES];
+      float mw[FEW_WAVES], lw[FEW_WAVES], f[FEW_WAVES];
       floatx4_t x[FEW_WAVES];
 #pragma unroll
       for (int w = 0; w < FEW_WAVES; ++w) {
@@ -653,11 +681,18 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
       }
 #pragma unroll
       for (int w = 0; w < FEW_WAVES; ++w) {
-        const float f = m == -INFINITY ? lw[w]   // (0, or a NaN)
-                                       : __builtin_amdgcn_exp2f(mw[w] - m);
-        l = fmaf(lw[w], f, l);
-        o4 += x[w] * f;
+        f[w] = m == -INFINITY ? lw[w]   // (0, or a NaN)
+                              : __builtin_amdgcn_exp2f(mw[w] - m);
+        l = fmaf(lw[w], f[w], l);
+        o4 += x[w] * f[w];
       }
+      if (const float y = fmaf(o4[0], o4[1], o4[2] * o4[3]); __builtin_expect(y != y, 0))
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          o4[i] = 0.f;
+#pragma unroll
+          for (int w = 0; w < FEW_WAVES; ++w) o4[i] += scaled(x[w][i], f[w]);
+        }
       write(pc.span * FEW_ROWS + r, r, m, l, ch, o4);
     }
     u += pc.units;
@@ -685,10 +720,6 @@ constexpr int MANY_WAVES = 8;
 constexpr int MANY_ROWS = 32 * MANY_WAVES;
 constexpr float kSlack = 8.f;
 
-template <int J>
-struct IntC {
-  static constexpr int value = J;
-};
 // max over the two halves of a wavefront that share a row (inline assembly: through the builtin the
 // compiler takes the two results of a swap of equal operands for equal; the s_nop covers the wait states
 // that a lane swap needs after a vector write of its operands)
@@ -732,7 +763,8 @@ struct ManyTile {
   static constexpr int POS_OFF = 2 * KEYS * T::ROW;
   static constexpr int BYTES = POS_OFF + KEYS * 4;
   static constexpr int ZERO_OFF = 4 * BYTES;           // a sub-tile's worth of V, zeros
-  static constexpr int SMEM = ZERO_OFF + SUB * T::ROW;
+  static constexpr int AGAIN_OFF = ZERO_OFF + SUB * T::ROW;
+  static constexpr int SMEM = AGAIN_OFF + 16;
 };
 
 template <int D, int TERMS, typename TO>
@@ -820,8 +852,10 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
       if (wave == 0 && sq.used > 0)
         dma4(p.kv_pos + sq.k0 + min(key0 + lane, sq.used - 1), dst + M::POS_OFF);
     };
+    int* const again = (int*)(smem + M::AGAIN_OFF);   // a wavefront wants the second pass
     if (n_subs > 0) {
       lds_barrier();   // the piece before has been read
+      if (tid == 0) *again = 0;
       request_tile(pc.t0, buf(pc.t0));
       if (pc.t0 + 1 < pc.t1) request_tile(pc.t0 + 1, buf(pc.t0 + 1));
     }
@@ -845,7 +879,6 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
                                            // term (keys 0..15, 16..31)
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) pb[1][k][0] = pb[1][k][1] = u32x4_t{0, 0, 0, 0};
-    bool pending = false;                  // O^T of the sub-tile before has not been added yet
 #pragma unroll
     for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
@@ -868,18 +901,16 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
       }
       return __builtin_bit_cast(uint4, v);
     };
-    // O^T of a sub-tile with nothing in between. ODD: V holds what is not finite, which reaches the rows
-    // that see it, and no other.
-    auto value_product = [&](auto parc, auto oddc, const char* sub) __attribute__((always_inline)) {
+    // O^T of a sub-tile with nothing in between. AGAIN: of the second pass, what is not finite by the bits of the
+    // scores whose keys the row sees.
+    auto value_product = [&](auto parc, auto againc, const char* sub, uint32_t seen_bits) __attribute__((always_inline)) {
       constexpr int par = decltype(parc)::value;
-      constexpr bool odd_v = decltype(oddc)::value != 0;
 #pragma unroll
       for (int cb = 0; cb < NCB; ++cb) {
         u32x4_t v[2];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) v[kb] = __builtin_bit_cast(u32x4_t, v_frag(sub, cb * 2 + kb));
-        if constexpr (odd_v) {
-          const u32x4_t t[2] = {pb[par][0][0], pb[par][0][1]};
+        if constexpr (decltype(againc)::value != 0) {
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
               floatx16_t sign;   // how many visible infinities of this sign (a NaN counts for both)
@@ -891,7 +922,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
                   a[x] = not_finite(v[kb][x], m == 1);
-                  seen[x] = ((t[kb][x] & 0xffffu) != 0 ? 0x3f80u : 0) | ((t[kb][x] >> 16) != 0 ? 0x3f800000u : 0);
+                  seen[x] = ones_of(seen_bits, kb * 8 + 2 * x);
                 }
                 sign = mfma32(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, seen), sign);
               }
@@ -922,8 +953,8 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
     auto needs_mask = [&](int st, int32_t pos) -> bool {   // (cached keys end before the tree's begin)
       return ((int)(__builtin_amdgcn_ballot_w64(pos > q_min) != 0) | (int)(st * SUB + SUB > sq.used)) != 0;
     };
-    // Masks the scores s[PAR] of sub-tile st; whether its V holds what is not finite.
-    auto mask = [&](auto parc, int st, const char* sub, const int32_t* pos) __attribute__((always_inline)) -> bool {
+    // Masks the scores s[PAR] of sub-tile st; bit i of the result: the row sees the key of score i.
+    auto mask = [&](auto parc, int st, const int32_t* pos) __attribute__((always_inline)) -> uint32_t {
       constexpr int PAR = decltype(parc)::value;
       const bool own = st >= n_cached;
       const int cnt = own ? sq.n - (st - n_cached) * SUB : sq.used - st * SUB;   // keys, if not SUB
@@ -936,6 +967,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
           see = (uint32_t)(p.mask[(int64_t)node * p.words + word] >> (((st - n_cached) & 1) * 32)) & there;
       }
       see >>= hf * 4;   // (bit a * 8 + i: score 4 a + i)
+      uint32_t seen_bits = 0;
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         const int4 x = *(const int4*)(pos + a * 8 + hf * 4);
@@ -944,15 +976,10 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
         for (int i = 0; i < 4; ++i) {
           const int vis = (int)((see & (1u << (a * 8 + i))) != 0) & ((int)own | (int)(kp[i] <= qp));
           s[PAR][4 * a + i] = vis != 0 ? s[PAR][4 * a + i] : -INFINITY;
+          seen_bits |= (uint32_t)vis << (4 * a + i);
         }
       }
-      uint32_t odd = 0;
-#pragma unroll
-      for (int i = 0; i < SUB * T::ROW / 1024; ++i) {
-        const uint4 x = *(const uint4*)(sub + M::V_OFF + i * 1024 + lane * 16);
-        odd |= any_not_finite(x.x) | any_not_finite(x.y) | any_not_finite(x.z) | any_not_finite(x.w);
-      }
-      return __builtin_amdgcn_ballot_w64(odd != 0) != 0;
+      return seen_bits;
     };
     // largest score of the row in s[PAR], log2 domain
     auto row_max = [&](auto parc) __attribute__((always_inline)) {
@@ -963,10 +990,10 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
       return halves_max(fmaxf(mx, s[PAR][15])) * p.scale_log2;
     };
 
-    // One step: softmax of sub-tile st (scores s[PAR], its rows and positions at `sub`, `pos`), products S^T
+    // One step: softmax of sub-tile st (scores s[PAR], its positions at `pos`), products S^T
     // of the next one (its K fragments on their way, the others at k_next) and O^T of the one before (V rows
     // at v_prev); the K fragments of the one after the next (k_after) are requested.
-    auto step = [&](auto parc, int st, const char* sub, const int32_t* pos, const char* k_next,
+    auto step = [&](auto parc, int st, const int32_t* pos, const char* k_next,
                     const int32_t* pos_next, const char* k_after, const char* v_prev) __attribute__((always_inline)) {
       constexpr int PAR = decltype(parc)::value;
       auto request = [&](int g) __attribute__((always_inline)) {
@@ -974,9 +1001,8 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
         else if (g < FRAGS) fr[g % AHEAD] = v_frag(v_prev, (g - NKS) % NCB * 2 + (g - NKS) / NCB);
         else fr[g % AHEAD] = k_frag(k_after, g - FRAGS);
       };
-      bool odd = false;
       if (__builtin_expect(masked, 0)) {
-        odd = mask(parc, st, sub, pos);
+        mask(parc, st, pos);
         top = row_max(parc);
       }
       const bool raise = top > ref + kSlack;
@@ -1064,8 +1090,6 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
 #pragma unroll
           for (int i = 0; i < 16; ++i) o_acc[cb][i] *= alpha;
       }
-      if (__builtin_expect(odd, 0)) value_product(parc, IntC<1>{}, sub);
-      pending = !odd;
     };
 
     if (n_subs > 0) {
@@ -1093,23 +1117,80 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
           masked = needs_mask(2 * pc.t0, pos_of(b)[rl]);
           top = row_max(IntC<0>{});
         }
-        const char* const zeros = smem + M::ZERO_OFF - M::V_OFF;   // (no product is pending: P times zeros)
+        const char* const zeros = smem + M::ZERO_OFF - M::V_OFF;   // (of the first step: P = 0 times zeros)
         for (int t = pc.t0; t < pc.t1; ++t) {
           const char* const b = buf(t);
           const char* const b_next = buf(t + 1);
-          step(IntC<0>{}, 2 * t, b, pos_of(b), b + HALF, pos_of(b) + SUB, b_next,
-               pending ? buf(t - 1) + HALF : zeros);
+          step(IntC<0>{}, 2 * t, pos_of(b), b + HALF, pos_of(b) + SUB, b_next,
+               t > pc.t0 ? buf(t - 1) + HALF : zeros);
           // (the next tile but one has landed everywhere, and the values of the one before have been read)
           landed_barrier();
           if (t + 3 < pc.t1) request_tile(t + 3, buf(t + 3));
           // (a second sub-tile that is not there holds copies of the last key, none of which counts)
-          step(IntC<1>{}, 2 * t + 1, b + HALF, pos_of(b) + SUB, b_next, pos_of(b_next), b_next + HALF,
-               pending ? b : zeros);
+          step(IntC<1>{}, 2 * t + 1, pos_of(b) + SUB, b_next, pos_of(b_next), b_next + HALF, b);
         }
-        if (pending) value_product(IntC<1>{}, IntC<0>{}, buf(pc.t1 - 1) + HALF);
+        value_product(IntC<1>{}, IntC<0>{}, buf(pc.t1 - 1) + HALF, 0);
+      }
+      l_run += xor32(l_run);
+      // (a row whose sum is a NaN is NaN in any case)
+      const float x = nan_of<NCB>(o_acc);
+      if (__builtin_amdgcn_ballot_w64(ok && l_run == l_run && x != x) != 0 && lane == 0) *again = 1;
+      lds_barrier();
+      if (__builtin_expect(__builtin_amdgcn_readfirstlane(*again) != 0, 0)) {
+        // The second pass, a tile after the other, by the arithmetic of the first.
+        ref = -INFINITY;
+        l_run = 0.f;
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o_acc[cb][i] = 0.f;
+        for (int st = 2 * pc.t0; st < min(2 * pc.t1, n_subs); ++st) {
+          if ((st & 1) == 0) {
+            lds_barrier();   // the tile before has been read
+            request_tile(st >> 1, smem);
+            landed_barrier();
+          }
+          if (!busy) continue;
+          const char* const b = smem + (st & 1) * HALF;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < NKS; ++ks)
+            s[0] = mfma32(__builtin_bit_cast(bf16x8_t, k_frag(b, ks)), __builtin_bit_cast(bf16x8_t, qf[ks]), s[0]);
+          const uint32_t seen_bits = mask(IntC<0>{}, st, pos_of(smem) + (st & 1) * SUB);
+          top = row_max(IntC<0>{});
+          float alpha = 1.f;
+          if (top > ref + kSlack) {
+            alpha = __builtin_amdgcn_exp2f(ref - top);
+            ref = top;
+          }
+          l_run *= alpha;
+#pragma unroll
+          for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o_acc[cb][i] = scaled(o_acc[cb][i], alpha);
+          const float use = ref == -INFINITY ? 0.f : ref;
+          float sum[2] = {0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            float e0 = __builtin_amdgcn_exp2f(fmaf(s[0][i], p.scale_log2, -use));
+            float e1 = __builtin_amdgcn_exp2f(fmaf(s[0][i + 1], p.scale_log2, -use));
+            sum[0] += e0;
+            sum[1] += e1;
+#pragma unroll
+            for (int k = 0; k < TERMS; ++k) {
+              const uint32_t y = pack_bf16(e0, e1);
+              pb[0][k][i >> 3][(i & 7) >> 1] = y;
+              e0 -= __builtin_bit_cast(float, y << 16);
+              e1 -= __builtin_bit_cast(float, y & 0xffff0000u);
+            }
+          }
+          l_run += sum[0] + sum[1];
+          value_product(IntC<0>{}, IntC<1>{}, b, seen_bits);
+        }
+        l_run += xor32(l_run);
       }
     }
-    l_run += xor32(l_run);
 
     // ---- the span's result, or this share's part of it ----
     if (ok) {
@@ -1174,45 +1255,63 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
   auto at = [&](int k) __attribute__((always_inline)) {
     return (int64_t)(2 * (w0 + k) + (k == 0 ? begins : 0)) * RM + (row - span * sq.rm);
   };
-  float m = -INFINITY, l = 0.f;
-  vec_t o = {};
-  for (int k0 = wave % W * CHUNK; k0 < n; k0 += 64) {
-    const int cnt = min(CHUNK, n - k0);
-    float mw = -INFINITY, lw = 0.f;
-    if (lane < cnt) {
-      const float2 x = *(const float2*)(p.part_ml + at(k0 + lane) * 2);
-      mw = x.x;
-      lw = x.y;
-    }
-    vec_t x[U];
-    auto rows = [&](int k) __attribute__((always_inline)) {
+  float m, l;
+  vec_t o;
+  auto pass = [&](auto againc) __attribute__((always_inline)) {
+    auto by = [](vec_t v, float w) __attribute__((always_inline)) {
+      if constexpr (decltype(againc)::value != 0) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = *(const vec_t*)(p.part_o + at(k0 + min(k + u, cnt - 1)) * D + lane * V);
+        for (int i = 0; i < V; ++i) v[i] = scaled(v[i], w);
+        return v;
+      } else {
+        return v * w;
+      }
     };
-    rows(0);
-    float top = mw;
+    m = -INFINITY;
+    l = 0.f;
+    o = vec_t{};
+    for (int k0 = wave % W * CHUNK; k0 < n; k0 += 64) {
+      const int cnt = min(CHUNK, n - k0);
+      float mw = -INFINITY, lw = 0.f;
+      if (lane < cnt) {
+        const float2 x = *(const float2*)(p.part_ml + at(k0 + lane) * 2);
+        mw = x.x;
+        lw = x.y;
+      }
+      vec_t x[U];
+      auto rows = [&](int k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int s = CHUNK / 2; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, CHUNK));
-    const float mn = fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, top))));
-    const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-    // (a part that saw nothing has weight 0; one that saw a NaN alone has no maximum and that sum)
-    const float f = lw == 0.f ? 0.f : mw == -INFINITY ? lw : __builtin_amdgcn_exp2f(mw - mn);
-    float sum = lw * f;
+        for (int u = 0; u < U; ++u) x[u] = *(const vec_t*)(p.part_o + at(k0 + min(k + u, cnt - 1)) * D + lane * V);
+      };
+      rows(0);
+      float top = mw;
 #pragma unroll
-    for (int s = CHUNK / 2; s > 0; s >>= 1) sum += __shfl_xor(sum, s, CHUNK);
-    l = fmaf(l, old, __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, sum))));
-    m = mn;
-    o *= old;
-    for (int k = 0; k < cnt; k += U) {
-      if (k > 0) rows(k);
+      for (int s = CHUNK / 2; s > 0; s >>= 1) top = fmaxf(top, __shfl_xor(top, s, CHUNK));
+      const float mn = fmaxf(m, __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, top))));
+      const float old = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      // (a part that saw nothing has weight 0; one that saw a NaN alone has no maximum and that sum)
+      const float f = lw == 0.f ? 0.f : mw == -INFINITY ? lw : __builtin_amdgcn_exp2f(mw - mn);
+      float sum = lw * f;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const float fu = k + u < cnt ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(
-                                           __builtin_bit_cast(int, f), k + u)) : 0.f;
-        if (k + u < cnt) o += x[u] * fu;
+      for (int s = CHUNK / 2; s > 0; s >>= 1) sum += __shfl_xor(sum, s, CHUNK);
+      l = fmaf(l, old, __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, sum))));
+      m = mn;
+      o = by(o, old);
+      for (int k = 0; k < cnt; k += U) {
+        if (k > 0) rows(k);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float fu = k + u < cnt ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(
+                                             __builtin_bit_cast(int, f), k + u)) : 0.f;
+          if (k + u < cnt) o += by(x[u], fu);
+        }
       }
     }
-  }
+  };
+  pass(IntC<0>{});
+  float y = o[0];
+  if constexpr (V > 1) y *= o[1];
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(y != y && l == l) != 0, 0)) pass(IntC<1>{});
   if constexpr (W > 1) {   // (all of a workgroup's wavefronts have come this far: one row)
     __shared__ vec_t other[W][64];
     __shared__ float2 ml[W];
@@ -1229,7 +1328,8 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
     for (int w = 0; w < W; ++w) {
       const float f = ml[w].y == 0.f ? 0.f : ml[w].x == -INFINITY ? ml[w].y : __builtin_amdgcn_exp2f(ml[w].x - top);
       l = fmaf(ml[w].y, f, l);
-      o += other[w][lane] * f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[i] += scaled(other[w][lane][i], f);
     }
     m = top;
   }
