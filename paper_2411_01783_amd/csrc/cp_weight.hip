@@ -134,7 +134,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_weight_kernel(const WeightParam
 #pragma unroll
   for (int f = 0; f < KB; ++f) {
     const int64_t key = (int64_t)sq.k0 + min(key0 + f * KEYS + rl, sq.used - 1);
-    kp[f] = p.kv_pos[key];
+    kp[f] = max(p.kv_pos[key], INT32_MIN + 1);   // (INT32_MIN is the position of rows that are none)
     const uint4* src = (const uint4*)((const TI*)p.k + key * tok_kv + kvh * D) + hf;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) kf[f][ks] = src[2 * ks];
@@ -180,14 +180,18 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_weight_kernel(const WeightParam
     }
     mine.advance(by_node, by_head, p.group);
   };
-  // a row that sees no key anywhere (LSE = -inf), and one behind the last, weighs nothing
+  // a row that sees no key anywhere (LSE = -inf), and one behind the last, is none: it weighs nothing
   auto put = [&](int to) {
+    if (st_lse == -INFINITY) {
+      st_lse = INFINITY;
+      st_pos = INT32_MIN;
+    }
 #pragma unroll
     for (int i = 0; i < ST; ++i) {
       const int r = i * RPI + tid / CH;
       *(uint4*)(tile[to] + r * ROW + (((tid % CH) ^ (r & (CH - 1))) << 4)) = st[i];
     }
-    lse_of[to][wave][lane] = st_lse == -INFINITY ? INFINITY : st_lse * kLog2e;
+    lse_of[to][wave][lane] = st_lse * kLog2e;
     pos_of[to][wave][lane] = st_pos;
   };
 
@@ -265,6 +269,7 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_weight_kernel(const WeightParam
     const int cur = t & 1;
     // which of the tile's rows see any of the wavefront's keys, and which not all
     const bool real = st_pos != INT32_MIN;
+    const uint64_t none = __builtin_amdgcn_ballot_w64(!real);
     const uint64_t some = __builtin_amdgcn_ballot_w64(real && st_pos >= k_min);
     const uint64_t hide = __builtin_amdgcn_ballot_w64(real && st_pos < k_max);
     __syncthreads();
@@ -282,7 +287,11 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_weight_kernel(const WeightParam
     auto term = [&](const floatx16_t& s, const floatx4_t (&lr)[4], int i) {
       return __builtin_amdgcn_exp2f(fmaf(s[i], p.scale_log2, -lr[i >> 2][i & 3]));
     };
+    bool masked = some != 0;
     if (KB > 1 && some != 0 && hide == 0) {
+      float before[KB];
+#pragma unroll
+      for (int f = 0; f < KB; ++f) before[f] = sum[f];
       constexpr int RB = TILE / 32, NB = RB * KB, PER = 16 / NKS > 0 ? 16 / NKS : 1;
       floatx16_t s[2];
       floatx4_t lr[RB][4];
@@ -319,7 +328,20 @@ __global__ __launch_bounds__(NW * 64, 2) void kv_weight_kernel(const WeightParam
         }
         if (j > 0) sum[(j - 1) % KB] += x[0] + x[1];
       }
-    } else if (some != 0) {
+      // A row that is none adds exp(-inf) = 0, or a NaN where its product with a key that is not finite is one: then
+      // the tile is done with its mask.
+      masked = false;
+      if (none != 0) {
+        bool nan = false;
+#pragma unroll
+        for (int f = 0; f < KB; ++f) nan |= sum[f] != sum[f];
+        masked = __builtin_amdgcn_ballot_w64(nan) != 0;
+        if (masked)
+#pragma unroll
+          for (int f = 0; f < KB; ++f) sum[f] = before[f];
+      }
+    }
+    if (__builtin_expect(masked, KB == 1)) {
 #pragma unroll
       for (int rb = 0; rb < TILE / 32; ++rb) {
         floatx4_t lr[4];
