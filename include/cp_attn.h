@@ -555,8 +555,8 @@ int cp_tree_mask(int32_t batch, const int32_t* cu_seqlens, const int32_t* parent
  *
  * bf16 and fp32, head_dim 64 and 128, any group of query heads. What a node does not see does not
  * reach it, NaN and infinity in hidden K and V rows included. Scores, statistics and accumulators
- * are fp32; with bf16 inputs the probabilities are rounded to bf16 where out is bf16, and keep 24 bits
- * where it is fp32. Two launches. Boundaries and counts on the device that contradict the shape
+ * are fp32; with bf16 inputs the probabilities are rounded to bf16 with head_dim 128 and a bf16 out only, else
+ * they keep 24 bits. Two launches. Boundaries and counts on the device that contradict the shape
  * are cut to it: nothing outside the tensors is read or written.
  * Errors: as cp_attn_partial; CP_ERR_NULL also for one of k_new, v_new without the other, CP_ERR_SHAPE also
  * for mask_words, and for total_q * n_q_heads or total_kv above INT32_MAX - 1024 or a batch above 2^24.

@@ -364,8 +364,9 @@ constexpr int few_smem() {
 // Bound by latencies: the chain {sequence boundaries} -> K, V, Q -> products -> join in LDS -> parts, and the
 // second launch; 8 nodes of 16 heads over 430 keys take 9 us here and 4 in the join, 32 sequences of 4096 keys at
 // 32 rows each 28.5 us (67 MB, 2.4 TB/s).
-// TI: K, V and Q. TO: O. P goes into the second product as TERMS bf16 terms (bf16 inputs): one
-// where O is rounded to bf16 itself, three (24 bits) where it stays fp32.
+// TI: K, V and Q. TO: O. P goes into the second product as TERMS bf16 terms (bf16 inputs): one at head_dim 128
+// where O is rounded to bf16 itself, three (24 bits) at head_dim 64, where cp_attn_partial keeps them too, and where O
+// stays fp32.
 template <typename TI, int D, int TERMS, typename TO>
 __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void tree_few_kernel(const TreeParams p) {
   using T = SubTile<TI, D>;
@@ -1578,7 +1579,7 @@ int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
                    : launch_few<float, 128, 1, bf16_t>(p, st);
   }
   if (s.head_dim == 64)
-    return f32_out ? launch_bf16<64, 3, float>(p, pl.many, st) : launch_bf16<64, 1, bf16_t>(p, pl.many, st);
+    return f32_out ? launch_bf16<64, 3, float>(p, pl.many, st) : launch_bf16<64, 3, bf16_t>(p, pl.many, st);
   return f32_out ? launch_bf16<128, 3, float>(p, pl.many, st) : launch_bf16<128, 1, bf16_t>(p, pl.many, st);
 }
 
