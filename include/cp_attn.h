@@ -577,7 +577,7 @@ int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
  *   dropped   (device) int32 or NULL: incremented by the number of rows that did not fit
  *   other arguments as cp_tree_attn and cp_kv_append. One launch, no workspace. k_new and v_new do
  *   not overlap the cache; calls on one cache are ordered by the caller, as cp_kv_append's.
- * Errors: as cp_kv_append, and CP_ERR_SHAPE for mask_words and for rows of more than 32 MB.
+ * Errors: as cp_kv_append, and CP_ERR_SHAPE for mask_words, rows of more than 32 MB and a batch above 2^23 - 1.
  */
 int cp_tree_accept(const cp_shape* shape, const void* k_new, const void* v_new,
                    const int32_t* pos_new, const int32_t* cu_seqlens_new, const uint64_t* tree_mask,

@@ -9,6 +9,16 @@ __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
   return x < lo ? lo : x > hi ? hi : x;
 }
 
+// Workgroups of one dimension, as a grid that can be launched: a dimension takes fewer than 2^32 threads, so more
+// than 2^22 workgroups go on in the second one. Those behind the last are the kernel's to end.
+inline dim3 wide_grid(int64_t blocks) {
+  constexpr int64_t row = 1 << 22;   // (of up to 1023 threads)
+  return blocks <= row ? dim3((unsigned)blocks) : dim3((unsigned)row, (unsigned)((blocks + row - 1) / row));
+}
+__device__ __forceinline__ int64_t wide_block() {
+  return (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+}
+
 // Inclusive prefix sums on the vector pipe (data-parallel moves between lanes; a __shfl is a round
 // trip through LDS): over 16 lanes, over the wavefront.
 template <int CTRL, int ROWS>

@@ -1234,7 +1234,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(const TreeParams p) {
   constexpr int V = D / 64, U = 8, CHUNK = 64 / W;
   typedef float vec_t __attribute__((ext_vector_type(V)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t idx = (int64_t)blockIdx.x * (4 / W) + wave / W;
+  const int64_t idx = wide_block() * (4 / W) + wave / W;
   if (idx >= p.total_q * p.n_q_heads) return;
   const int node = (uint32_t)idx / (uint32_t)p.n_q_heads;
   const int head = (int)idx - node * p.n_q_heads, kvh = (uint32_t)head / (uint32_t)p.group;
@@ -1451,9 +1451,9 @@ template <int D, int RM, int SPT, typename TO>
 int launch_join(const TreeParams& p, hipStream_t st) {
   const int64_t rows = p.total_q * p.n_q_heads;
   if (rows <= kJoinRows)
-    hipLaunchKernelGGL((tree_join_kernel<D, RM, SPT, 4, TO>), dim3((unsigned)rows), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((tree_join_kernel<D, RM, SPT, 4, TO>), wide_grid(rows), dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((tree_join_kernel<D, RM, SPT, 1, TO>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((tree_join_kernel<D, RM, SPT, 1, TO>), wide_grid((rows + 3) / 4), dim3(256), 0, st, p);
   return check_launch();
 }
 
@@ -1604,6 +1604,8 @@ int cp_tree_accept(const cp_shape* shape, const void* k_new, const void* v_new,
     return CP_ERR_NULL;
   if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) || !aligned16(v_cache))
     return CP_ERR_ALIGN;
+  // the grid's threads
+  if (s.batch > INT32_MAX / ACCEPT_THREADS) return CP_ERR_SHAPE;
   if (s.total_q == 0) return CP_OK;
   AcceptParams p;
   p.k_new = (const uint4*)k_new; p.v_new = (const uint4*)v_new;

@@ -398,9 +398,10 @@ __global__ __launch_bounds__(256) void kv_weight_sum_kernel(const WeightParams p
   int begin = 0;
   Seq sq;
   const int per = p.wg_keys / SUM_KEYS;
-  if (find_block(p, blockIdx.x / per, &begin, &sq) < 0) return;
+  const int x = (int)wide_block();
+  if (find_block(p, x / per, &begin, &sq) < 0) return;
   const int lane = threadIdx.x & 63, quarter = threadIdx.x >> 6;
-  const int key = ((int)blockIdx.x / per - begin) * p.wg_keys + (int)blockIdx.x % per * SUM_KEYS + lane;
+  const int key = (x / per - begin) * p.wg_keys + x % per * SUM_KEYS + lane;
   const int64_t at = (int64_t)sq.k0 + min(key, sq.used - 1);
   const int n = p.n_ranges * p.n_kv_heads;
   const float old = quarter == 0 && p.decay != 0.f ? p.weight[at] : 0.f;
@@ -521,7 +522,6 @@ extern "C" int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int
 #undef CP_WEIGHT
   if (check_launch() != CP_OK) return CP_ERR_LAUNCH;
   if (p.part == nullptr) return CP_OK;
-  hipLaunchKernelGGL(kv_weight_sum_kernel, dim3((unsigned)(pl.blocks * (p.wg_keys / SUM_KEYS))), dim3(256), 0,
-                     st, p);
+  hipLaunchKernelGGL(kv_weight_sum_kernel, wide_grid(pl.blocks * (p.wg_keys / SUM_KEYS)), dim3(256), 0, st, p);
   return check_launch();
 }

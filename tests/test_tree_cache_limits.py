@@ -1,0 +1,24 @@
+"""Sizes at which the calls on the KV cache are refused, without a GPU."""
+import ctypes
+
+from paper_2411_01783_amd import binding as B
+
+ONE = ctypes.c_void_p(256)    # never dereferenced: the calls below fail validation first
+SHAPE = -2
+
+
+def shape(**kw):
+    a = dict(dtype=B.CP_BF16, head_dim=128, n_q_heads=16, n_kv_heads=2, total_q=8, total_kv=64, batch=2)
+    a.update(kw)
+    return B.make_shape(**a)
+
+
+def accept(s):
+    return B.load().cp_tree_accept(ctypes.byref(s), ONE, ONE, ONE, ONE, ONE, 1, ONE, ONE, ONE, ONE, ONE, ONE, None,
+                                   None)
+
+
+def test_paths_of_more_sequences_than_a_grid_holds():
+    assert accept(shape(batch=2**23)) == SHAPE
+    assert accept(shape(batch=2**31 - 1)) == SHAPE
+    assert accept(shape(batch=2**23 - 1, total_q=0)) == 0
