@@ -591,7 +591,8 @@ extern "C" int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, 
     return CP_ERR_NULL;
   if (!aligned16(k_cache) || !aligned16(v_cache) || !aligned16(k_to) || !aligned16(v_to))
     return CP_ERR_ALIGN;
-  if (s.batch > 65535) return CP_ERR_SHAPE;   // the grid's second dimension
+  static_assert(kMaxWalkedBatch <= 65535, "the grid's second dimension");
+  if (s.batch > kMaxWalkedBatch) return CP_ERR_SHAPE;
   const EvictPlan pl = evict_plan(s);
   if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 || workspace_bytes < pl.bytes)
     return CP_ERR_WORKSPACE;

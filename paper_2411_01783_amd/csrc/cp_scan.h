@@ -9,6 +9,10 @@ __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
   return x < lo ? lo : x > hi ? hi : x;
 }
 
+// Sequences of a call whose workgroups (and, of trees, rows) all walk the batch, 64 sequences a step: beyond it that walk
+// is what a call does (at 2^20 sequences of one node it would be half a minute).
+constexpr int32_t kMaxWalkedBatch = 65535;
+
 // Workgroups of one dimension, as a grid that can be launched: a dimension takes fewer than 2^32 threads, so more
 // than 2^22 workgroups go on in the second one. Those behind the last are the kernel's to end.
 inline dim3 wide_grid(int64_t blocks) {

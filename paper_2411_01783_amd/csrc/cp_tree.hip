@@ -1550,10 +1550,10 @@ int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
   if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) ||
       !aligned16(v_cache) || !aligned16(out))
     return CP_ERR_ALIGN;
+  if (s.batch > kMaxWalkedBatch) return CP_ERR_SHAPE;
   if (s.total_q == 0) return CP_OK;
   // rows of the merge's grid, nodes and tokens of a sequence with their sub-tiles are kept in 31 bits
-  if (s.total_q * s.n_q_heads > INT32_MAX - 1024 || s.total_kv > INT32_MAX - 1024 || s.batch > (1 << 24))
-    return CP_ERR_SHAPE;
+  if (s.total_q * s.n_q_heads > INT32_MAX - 1024 || s.total_kv > INT32_MAX - 1024) return CP_ERR_SHAPE;
   const TreePlan pl = tree_plan(s);
   if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 ||
       workspace_bytes < pl.o_bytes + pl.ml_bytes)

@@ -485,6 +485,7 @@ extern "C" int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int
   if (s.total_kv > 0 && (k_cache == nullptr || kv_pos_cache == nullptr || weight == nullptr))
     return CP_ERR_NULL;
   if (!aligned16(q) || !aligned16(k_cache)) return CP_ERR_ALIGN;
+  if (s.batch > kMaxWalkedBatch) return CP_ERR_SHAPE;
   if (s.total_kv == 0) return CP_OK;
   // key indices and rows in 31 bits
   if (s.total_kv > INT32_MAX - 256 || s.total_q * s.n_q_heads > INT32_MAX - TILE) return CP_ERR_SHAPE;

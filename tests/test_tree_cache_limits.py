@@ -22,3 +22,21 @@ def test_paths_of_more_sequences_than_a_grid_holds():
     assert accept(shape(batch=2**23)) == SHAPE
     assert accept(shape(batch=2**31 - 1)) == SHAPE
     assert accept(shape(batch=2**23 - 1, total_q=0)) == 0
+
+
+def tree(s):
+    return B.load().cp_tree_attn(ctypes.byref(s), ONE, ONE, ONE, ONE, ONE, ONE, 1, ONE, ONE, ONE, ONE, ONE, ONE, ONE, 0,
+                                 ONE, ctypes.c_size_t(1 << 62), None)
+
+
+def weight(s):
+    return B.load().cp_kv_attn_weight(ctypes.byref(s), ONE, ONE, ONE, ONE, ONE, ONE, ONE, ONE, 1.0, ONE, ONE,
+                                      ctypes.c_size_t(1 << 62), None)
+
+
+def test_batches_that_a_walk_would_not_end_in():
+    for batch in (65536, 2**24, 2**31 - 1):
+        assert tree(shape(batch=batch)) == SHAPE
+        assert weight(shape(batch=batch)) == SHAPE
+    assert tree(shape(batch=65535, total_q=0)) == 0
+    assert weight(shape(batch=65535, total_kv=0)) == 0
