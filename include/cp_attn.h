@@ -630,7 +630,8 @@ int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int32_t* q_pos
  * Two launches, or seven where the sequences have more than 24576 slots on average. The result does not
  * depend on the order in which anything runs; calls on one cache are ordered by the caller.
  * Errors: as cp_kv_append; CP_ERR_NULL for part of a destination, CP_ERR_SHAPE for sinks below 0, a batch above 65535,
- * slots_to outside 0 .. INT32_MAX, or a destination that is the source; CP_ERR_WORKSPACE.
+ * total_kv or slots_to above INT32_MAX - 262144, slots_to below 0, or a destination that is the source;
+ * CP_ERR_WORKSPACE.
  */
 int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, int32_t* kv_pos_cache,
                 float* weight, const int32_t* cu_seqlens_kv, int32_t* seq_used,

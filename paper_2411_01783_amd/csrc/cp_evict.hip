@@ -62,6 +62,7 @@ constexpr int BINS = 2048;
 // Slots of a chunk. More chunks are read in fewer rounds but add more counts up: us for 8192, 4096 and 2048, 4 sequences of
 // 32768 slots 42, 34, 30, 16 of 65536 47, 39, 44, 64 of 32768 60, 64, 78.
 constexpr int CHUNK = 4096;
+constexpr int64_t kMaxSlots = INT32_MAX - 64 * CHUNK;   // slots, and the ends of steps over them, are counted in 31 bits
 constexpr int HIST = 3 * BINS + 64;       // three digits' counts, and the number of protected slots
 
 // Order-preserving key of a weight; protected slots are above all, NaN below all.
@@ -322,7 +323,7 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
     // ... then their ranks
     Ranks r = {0, 0, 0}, end = {0, 0, 0};
     {
-      const int w0 = min(sq.n, lane * part), w1 = min(sq.n, w0 + part);
+      const int w0 = min(sq.n, min(lane, SEL_WAVES) * part), w1 = min(sq.n, w0 + part);
       add_parts(lane < SEL_WAVES, lane < SEL_WAVES ? *(const int4*)counts[lane] : make_int4(0, 0, 0, 0), w0, w1,
                 keep, ties, wave, r, SEL_WAVES, end);
     }
@@ -519,7 +520,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
     }
   }
   if (!p.in_place)
-    for (int64_t i = keep + first; i < to.room; i += stride) {
+    for (int64_t i = (int64_t)keep + first; i < to.room; i += stride) {
       p.pos_to[d0 + i] = CP_POS_PAD_KV;
       p.weight_to[d0 + i] = 0.f;
     }
@@ -568,7 +569,7 @@ extern "C" int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, 
   const int rc = check_cache_shape(shape);
   if (rc != CP_OK) return rc;
   const cp_shape& s = *shape;
-  if (sinks < 0) return CP_ERR_SHAPE;
+  if (sinks < 0 || s.total_kv > kMaxSlots) return CP_ERR_SHAPE;
   if (cu_seqlens_kv == nullptr || seq_used == nullptr || budget == nullptr) return CP_ERR_NULL;
   const bool in_place = k_to == nullptr;
   if (in_place) {
@@ -581,7 +582,7 @@ extern "C" int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, 
     if (v_to == nullptr || kv_pos_to == nullptr || weight_to == nullptr || cu_seqlens_to == nullptr ||
         seq_used_to == nullptr)
       return CP_ERR_NULL;
-    if (slots_to < 0 || slots_to > INT32_MAX) return CP_ERR_SHAPE;
+    if (slots_to < 0 || slots_to > kMaxSlots) return CP_ERR_SHAPE;
     if (k_to == k_cache || v_to == v_cache || kv_pos_to == kv_pos_cache || weight_to == weight ||
         seq_used_to == seq_used)
       return CP_ERR_SHAPE;  // another cache, or in place

@@ -4,7 +4,7 @@ import ctypes
 from paper_2411_01783_amd import binding as B
 
 ONE = ctypes.c_void_p(256)    # never dereferenced: the calls below fail validation first
-SHAPE = -2
+SHAPE, WORKSPACE = -2, -4
 
 
 def shape(**kw):
@@ -40,3 +40,19 @@ def test_batches_that_a_walk_would_not_end_in():
         assert weight(shape(batch=batch)) == SHAPE
     assert tree(shape(batch=65535, total_q=0)) == 0
     assert weight(shape(batch=65535, total_kv=0)) == 0
+
+
+def evict(s, slots_to=None):
+    to = [None] * 6 + [0] if slots_to is None else [ctypes.c_void_p(4096)] * 6 + [slots_to]
+    return B.load().cp_kv_evict(ctypes.byref(s), ONE, ONE, ONE, ONE, ONE, ONE, ONE, None, 0, *to, None, ctypes.c_size_t(0),
+                                None)
+
+
+def test_evictions_whose_slots_pass_31_bits():
+    """Steps over the slots end up to 2^18 behind the last: those of larger caches would have wrapped, and the cache
+    of a sequence of nearly 2^31 tokens been given up."""
+    most = 2**31 - 1 - 2**18
+    for slots in (most + 1, 2**31 - 1):
+        assert evict(shape(head_dim=8, n_q_heads=1, n_kv_heads=1, batch=1, total_kv=slots)) == SHAPE
+        assert evict(shape(), slots) == SHAPE
+    assert evict(shape(total_kv=most)) == WORKSPACE and evict(shape(), most) == WORKSPACE   # (there is none)
