@@ -559,7 +559,8 @@ int cp_tree_mask(int32_t batch, const int32_t* cu_seqlens, const int32_t* parent
  * they keep 24 bits. Two launches. Boundaries and counts on the device that contradict the shape
  * are cut to it: nothing outside the tensors is read or written.
  * Errors: as cp_attn_partial; CP_ERR_NULL also for one of k_new, v_new without the other, CP_ERR_SHAPE also
- * for mask_words, a batch above 65535, and total_q * n_q_heads or total_kv above INT32_MAX - 1024.
+ * for mask_words, a batch above 65535, total_q * n_q_heads or total_q + total_kv above INT32_MAX - 1024, and
+ * n_q_heads * head_dim above INT32_MAX.
  */
 int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
                  const int32_t* cu_seqlens_q, const void* k_new, const void* v_new,
@@ -603,7 +604,8 @@ int cp_tree_accept(const cp_shape* shape, const void* k_new, const void* v_new,
  * bf16 and fp32, head_dim 64 and 128, any group of query heads. fp32 arithmetic, sums in a fixed
  * order. What a query does not see does not reach the sum. One launch, or two with a workspace.
  * Errors: as cp_attn_partial, and CP_ERR_SHAPE for a negative, infinite or NaN decay, a batch above 65535, total_kv
- * above INT32_MAX - 256, total_q * n_q_heads above INT32_MAX - 64, or more than 65535 KV heads.
+ * above INT32_MAX - 256, total_q * n_q_heads above INT32_MAX - 64, n_q_heads * head_dim above INT32_MAX, or more
+ * than 65535 KV heads.
  */
 int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int32_t* q_pos,
                       const int32_t* cu_seqlens_q, const float* lse, const void* k_cache,

@@ -1552,8 +1552,10 @@ int cp_tree_attn(const cp_shape* shape, const void* q, const int32_t* q_pos,
     return CP_ERR_ALIGN;
   if (s.batch > kMaxWalkedBatch) return CP_ERR_SHAPE;
   if (s.total_q == 0) return CP_OK;
-  // rows of the merge's grid, nodes and tokens of a sequence with their sub-tiles are kept in 31 bits
-  if (s.total_q * s.n_q_heads > INT32_MAX - 1024 || s.total_kv > INT32_MAX - 1024) return CP_ERR_SHAPE;
+  // rows, a token's channels, and a sequence's tokens and nodes in one line are counted in 31 bits
+  if (s.total_q * s.n_q_heads > INT32_MAX - 1024 || s.total_kv + s.total_q > INT32_MAX - 1024 ||
+      (int64_t)s.n_q_heads * s.head_dim > INT32_MAX)
+    return CP_ERR_SHAPE;
   const TreePlan pl = tree_plan(s);
   if (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 ||
       workspace_bytes < pl.o_bytes + pl.ml_bytes)

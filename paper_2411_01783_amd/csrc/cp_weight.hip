@@ -487,8 +487,10 @@ extern "C" int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int
   if (!aligned16(q) || !aligned16(k_cache)) return CP_ERR_ALIGN;
   if (s.batch > kMaxWalkedBatch) return CP_ERR_SHAPE;
   if (s.total_kv == 0) return CP_OK;
-  // key indices and rows in 31 bits
-  if (s.total_kv > INT32_MAX - 256 || s.total_q * s.n_q_heads > INT32_MAX - TILE) return CP_ERR_SHAPE;
+  // key indices, rows and a token's channels in 31 bits
+  if (s.total_kv > INT32_MAX - 256 || s.total_q * s.n_q_heads > INT32_MAX - TILE ||
+      (int64_t)s.n_q_heads * s.head_dim > INT32_MAX)
+    return CP_ERR_SHAPE;
   const WeightPlan pl = weight_plan(s);
   if (pl.bytes > 0 && (workspace == nullptr || ((uintptr_t)workspace & 255u) != 0 ||
                        workspace_bytes < pl.bytes))

@@ -56,3 +56,12 @@ def test_evictions_whose_slots_pass_31_bits():
         assert evict(shape(head_dim=8, n_q_heads=1, n_kv_heads=1, batch=1, total_kv=slots)) == SHAPE
         assert evict(shape(), slots) == SHAPE
     assert evict(shape(total_kv=most)) == WORKSPACE and evict(shape(), most) == WORKSPACE   # (there is none)
+
+
+def test_tokens_and_channels_that_pass_31_bits():
+    # a tree's own keys are counted on behind the cached ones
+    assert tree(shape(total_q=1000, total_kv=2**31 - 1 - 1024 - 999)) == SHAPE
+    # heads times head_dim of one token
+    for heads in (dict(n_q_heads=2**24, n_kv_heads=1), dict(n_q_heads=2**25, n_kv_heads=2**10)):
+        assert tree(shape(total_q=1, **heads)) == SHAPE
+        assert weight(shape(total_q=1, **heads)) == SHAPE
