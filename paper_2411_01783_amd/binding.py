@@ -295,7 +295,7 @@ def _ws_ptr(ws: Optional[torch.Tensor]):
     if ws is None:
         return None, 0
     p = (ws.data_ptr() + 255) & ~255
-    return p, ws.numel() - (p - ws.data_ptr())
+    return p, max(0, ws.numel() - (p - ws.data_ptr()))
 
 
 def cp_attn_partial(q, k, v, q_pos, kv_pos, cu_seqlens_q=None, cu_seqlens_kv=None,

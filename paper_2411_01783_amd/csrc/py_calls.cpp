@@ -94,8 +94,9 @@ struct Workspace {
   size_t bytes = 0;
   void set(const at::Tensor& t) {
     const uintptr_t p = (uintptr_t)t.const_data_ptr(), a = (p + 255) & ~(uintptr_t)255;
+    const int64_t left = t.numel() - (int64_t)(a - p);
     ptr = (void*)a;
-    bytes = (size_t)(t.numel() - (int64_t)(a - p));
+    bytes = left > 0 ? (size_t)left : 0;   // (one that ends in front of its first aligned byte holds nothing)
   }
 };
 void use_workspace(Workspace& w, PyObject* given, const cp_shape& s, int32_t kind,
