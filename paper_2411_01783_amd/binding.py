@@ -23,6 +23,7 @@ CP_BF16, CP_FP32 = 0, 1
 CP_WS_PARTIAL, CP_WS_DECODE, CP_WS_MERGE = 0, 1, 2
 CP_WS_TREE, CP_WS_WEIGHT, CP_WS_EVICT = 3, 4, 5
 CP_TREE_MAX_WORDS = 16
+CP_ERR_SHAPE = -2
 CP_POS_PAD_KV = 2**31 - 1
 CP_POS_PAD_Q = -1
 CP_MAX_PARTS = 64
@@ -416,6 +417,8 @@ def cp_tree_mask(parents, cu_seqlens, words: Optional[int] = None) -> np.ndarray
         raise ValueError("parents and cu_seqlens do not match")
     if words is None:
         words = max(1, (int(np.diff(cu).max()) + 63) // 64)
+    if not 1 <= words <= CP_TREE_MAX_WORDS:
+        raise CpError(CP_ERR_SHAPE, "cp_tree_mask")
     mask = np.zeros((parents.size, words), dtype=np.int64)
     at = ctypes.POINTER(_i32)
     _check(load().cp_tree_mask(cu.size - 1, cu.ctypes.data_as(at), parents.ctypes.data_as(at), words,

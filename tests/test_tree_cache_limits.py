@@ -1,6 +1,9 @@
 """Sizes at which the calls on the KV cache are refused, without a GPU."""
 import ctypes
 
+import numpy as np
+import pytest
+
 from paper_2411_01783_amd import binding as B
 
 ONE = ctypes.c_void_p(256)    # never dereferenced: the calls below fail validation first
@@ -65,3 +68,11 @@ def test_tokens_and_channels_that_pass_31_bits():
     for heads in (dict(n_q_heads=2**24, n_kv_heads=1), dict(n_q_heads=2**25, n_kv_heads=2**10)):
         assert tree(shape(total_q=1, **heads)) == SHAPE
         assert weight(shape(total_q=1, **heads)) == SHAPE
+
+
+def test_trees_of_more_nodes_than_words_have_bits_for():
+    # refused before there is a mask of that many words (125 GB of them here)
+    nodes = 1000000
+    with pytest.raises(B.CpError) as e:
+        B.cp_tree_mask(np.full(nodes, -1, dtype=np.int32), [0, nodes])
+    assert e.value.status == SHAPE
