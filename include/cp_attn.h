@@ -620,8 +620,9 @@ int cp_kv_attn_weight(const cp_shape* shape, const void* q, const int32_t* q_pos
  * never protected), then by weight, ties to the lowest slot; a NaN counts as the lowest weight.
  * Kept tokens in slots 0 .. keep-1 of the sequence's range stay in their slot, and the i-th kept token
  * behind them takes the i-th slot that became free among them. (The order of the slots means
- * nothing to attention, which goes by kv_pos.) Slots behind the kept tokens get CP_POS_PAD_KV and
- * weight 0; their K and V are left as they were.
+ * nothing to attention, which goes by kv_pos.) Slots that a token leaves, and all slots of another cache behind the
+ * kept tokens, get CP_POS_PAD_KV and weight 0; in place the slots from seq_used[b] on are not touched. K and V
+ * of unused slots are left as they were (cp_attn_decode needs them finite).
  *   shape     dtype, head_dim, n_kv_heads, batch, total_kv (slots) as in cp_kv_append
  *   budget    (device) int32 [batch]; below 0 counts as 0
  *   protect_from (device) int32 [batch] or NULL (no token is protected for being recent)

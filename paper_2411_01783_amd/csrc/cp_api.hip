@@ -30,17 +30,12 @@ int check_cache_shape(const cp_shape* s) {
   if (s->head_dim < 8 || s->head_dim > 256 || s->head_dim % 8 != 0) return CP_ERR_UNSUPPORTED;
   if (s->n_kv_heads < 1 || s->batch < 1 || s->total_q < 0 || s->total_kv < 0) return CP_ERR_SHAPE;
   if (s->total_q > INT32_MAX || s->total_kv > INT32_MAX) return CP_ERR_SHAPE;
-  // 16-byte chunks of a row are counted in 31 bits
-  if ((int64_t)s->n_kv_heads * s->head_dim > INT32_MAX / 4) return CP_ERR_SHAPE;
   return CP_OK;
 }
 
 }  // namespace cp
 
 namespace {
-
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-inline bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
 
 inline float resolve_scale(float scale, int head_dim) {
   return scale > 0.f ? scale : 1.0f / sqrtf((float)head_dim);

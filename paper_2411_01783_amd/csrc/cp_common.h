@@ -54,10 +54,13 @@ __device__ __forceinline__ int touch_arguments() {
   return x;
 }
 
-// ---- launchers (each returns a cp_status; enqueue on `stream` only) ----
+// ---- checks of arguments, workspaces ----
 
-// fp32 vector kernel: any supported dtype / head_dim, packed batches.
-// Argument checks on a shape: of an attention call, of a call on the KV cache alone (cp_api.hip).
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+inline bool aligned256(const void* p) { return ((uintptr_t)p & 255u) == 0; }
+inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+// A shape of an attention call, of a call on the KV cache alone (cp_api.hip).
 int check_shape(const cp_shape* s);
 int check_cache_shape(const cp_shape* s);
 
@@ -66,6 +69,9 @@ size_t tree_workspace_bytes(const cp_shape& s);
 size_t weight_workspace_bytes(const cp_shape& s);
 size_t evict_workspace_bytes(const cp_shape& s);
 
+// ---- launchers (each returns a cp_status; enqueue on `stream` only) ----
+
+// fp32 vector kernel: any supported dtype / head_dim, packed batches.
 int launch_partial_generic(const cp_shape& s, float scale, const void* q, const void* k,
                            const void* v, const int32_t* q_pos, const int32_t* kv_pos,
                            const int32_t* cu_q, const int32_t* cu_kv, void* out, float* lse,

@@ -75,7 +75,6 @@ __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-
 __global__ __launch_bounds__(NTHREADS, 2) void decode_kernel(Params p) {
   extern __shared__ __align__(16) char smem[];
   const int tid = threadIdx.x;
@@ -1130,8 +1129,6 @@ __global__ __launch_bounds__(OW * 64) void decode_flat_merge_one_kernel(const Fl
   if (lse_out != nullptr && tid == 0 && col == 0)
     lse_out[row] = den > 0.f ? lmax + __logf(den) : -INFINITY;
 }
-
-inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Power-of-two split count: about 512 workgroups in total (two per CU, all resident at
 // once), at least 128 keys per split on average.

@@ -527,9 +527,6 @@ __global__ __launch_bounds__(256) void evict_move_kernel(const EvictParams p) {
   if (first == 0) p.used_to[b] = keep;
 }
 
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 // Above this many slots a sequence, on average, they are cut into chunks. us (a workgroup each, chunks): 4 sequences
 // of 8192 slots 19 and 34, of 16384 29 and 34, of 32768 48 and 34, of 131072 232 and 35; 64 of 16384 43 and 50,
 // of 32768 63 and 64, of 65536 139 and 103.
@@ -570,6 +567,8 @@ extern "C" int cp_kv_evict(const cp_shape* shape, void* k_cache, void* v_cache, 
   if (rc != CP_OK) return rc;
   const cp_shape& s = *shape;
   if (sinks < 0 || s.total_kv > kMaxSlots) return CP_ERR_SHAPE;
+  // 16-byte chunks of a row are counted in 31 bits
+  if ((int64_t)s.n_kv_heads * s.head_dim > INT32_MAX / 4) return CP_ERR_SHAPE;
   if (cu_seqlens_kv == nullptr || seq_used == nullptr || budget == nullptr) return CP_ERR_NULL;
   const bool in_place = k_to == nullptr;
   if (in_place) {

@@ -4,7 +4,7 @@
 //
 // Layout: packed [slots, n_kv_heads, head_dim] with sequence b owning the slot range
 // [cu_kv[b], cu_kv[b+1]) (its capacity on this rank). The first used[b] slots hold tokens, in
-// the order they arrived; every other slot carries CP_POS_PAD_KV in the position array, which
+// the order they arrived until an eviction moves some; every other slot carries CP_POS_PAD_KV in the position array, which
 // no query position can reach, so the attention kernels read the cache as it is.
 //
 // Pure data movement, HBM-bound: one 16-byte chunk of K and of V per thread.
@@ -114,8 +114,6 @@ __global__ __launch_bounds__(256) void kv_cache_reset_kernel(uint4* k_cache, uin
   if (t == 0 && dropped != nullptr) *dropped = 0;
 }
 
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
 }  // namespace
 }  // namespace cp
 
@@ -124,11 +122,10 @@ extern "C" {
 int cp_kv_cache_reset(const cp_shape* shape, void* k_cache, void* v_cache,
                       int32_t* kv_pos_cache, int32_t* seq_used, int32_t* dropped, void* stream) {
   if (shape == nullptr) return CP_ERR_NULL;
-  const cp_shape& s = *shape;
-  if (s.dtype != CP_BF16 && s.dtype != CP_FP32) return CP_ERR_UNSUPPORTED;
-  if (s.head_dim < 8 || s.head_dim > 256 || s.head_dim % 8 != 0) return CP_ERR_UNSUPPORTED;
-  if (s.n_kv_heads < 1 || s.batch < 1 || s.total_kv < 0 || s.total_kv > INT32_MAX)
-    return CP_ERR_SHAPE;
+  cp_shape s = *shape;
+  s.total_q = 0;   // (not read)
+  const int rc = cp::check_cache_shape(&s);
+  if (rc != CP_OK) return rc;
   if (seq_used == nullptr) return CP_ERR_NULL;
   if (s.total_kv > 0 && (k_cache == nullptr || v_cache == nullptr || kv_pos_cache == nullptr))
     return CP_ERR_NULL;
@@ -148,12 +145,9 @@ int cp_kv_append(const cp_shape* shape, const void* k_new, const void* v_new,
                  const int32_t* pos_new, const int32_t* cu_seqlens_new, void* k_cache,
                  void* v_cache, int32_t* kv_pos_cache, const int32_t* cu_seqlens_kv,
                  int32_t* seq_used, int32_t* dropped, void* stream) {
-  if (shape == nullptr) return CP_ERR_NULL;
+  const int rc = cp::check_cache_shape(shape);
+  if (rc != CP_OK) return rc;
   const cp_shape& s = *shape;
-  if (s.dtype != CP_BF16 && s.dtype != CP_FP32) return CP_ERR_UNSUPPORTED;
-  if (s.head_dim < 8 || s.head_dim > 256 || s.head_dim % 8 != 0) return CP_ERR_UNSUPPORTED;
-  if (s.n_kv_heads < 1 || s.batch < 1 || s.total_q < 0 || s.total_kv < 0) return CP_ERR_SHAPE;
-  if (s.total_kv > INT32_MAX || s.total_q > INT32_MAX) return CP_ERR_SHAPE;
   if (cu_seqlens_new == nullptr || cu_seqlens_kv == nullptr || seq_used == nullptr)
     return CP_ERR_NULL;
   if (s.total_q == 0) return CP_OK;

@@ -170,8 +170,6 @@ __device__ __forceinline__ void wave_lds_fence() {
 
 #include "cp_prefill_pipe.h"
 
-inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 // Split count of the KV axis for `wgs` workgroups of 256 rows over `tiles` tiles.
 // Splitting starts below 256 workgroups, one per CU. Cost of a split count, in units of one
 // tile step of a workgroup: the workgroups run in rounds of 256, each round walks its tiles plus

@@ -1405,9 +1405,6 @@ __global__ __launch_bounds__(ACCEPT_THREADS) void tree_accept_kernel(const Accep
   }
 }
 
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 constexpr int64_t kFewBlocks = 1 << 26, kFewOneBlock = 1 << 27, kFewTiles = 768;
 struct TreePlan {
   bool many;

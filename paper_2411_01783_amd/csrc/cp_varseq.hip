@@ -21,8 +21,6 @@
 namespace cp {
 namespace {
 
-inline size_t round256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 constexpr int kScanHere = 1024;  // batches up to this size: the encode kernel scans the spans
 constexpr int kBatchHere = 64;   // a lane each scans the spans (encode_in_one_launch takes fewer)
 

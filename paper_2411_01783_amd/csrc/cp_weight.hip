@@ -460,8 +460,6 @@ WeightPlan weight_plan(const cp_shape& s) {
   return pl;
 }
 
-inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-
 }  // namespace
 
 size_t weight_workspace_bytes(const cp_shape& s) {
