@@ -323,7 +323,8 @@ __global__ __launch_bounds__(SEL_THREADS) void evict_select_kernel(const EvictPa
     // ... then their ranks
     Ranks r = {0, 0, 0}, end = {0, 0, 0};
     {
-      const int w0 = min(sq.n, min(lane, SEL_WAVES) * part), w1 = min(sq.n, w0 + part);
+      // (unsigned: of the lanes that stand for no wavefront the product may wrap)
+      const int w0 = (int)min((uint32_t)sq.n, (uint32_t)lane * part), w1 = min(sq.n, w0 + part);
       add_parts(lane < SEL_WAVES, lane < SEL_WAVES ? *(const int4*)counts[lane] : make_int4(0, 0, 0, 0), w0, w1,
                 keep, ties, wave, r, SEL_WAVES, end);
     }
