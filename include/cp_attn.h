@@ -34,9 +34,9 @@
  *     carries CP_POS_PAD_Q.
  *   - What a query does not see does not reach it: a NaN or infinity in another
  *     query, in a padded one, or in a hidden K row. In cp_attn_partial,
- *     cp_attn_partial_accumulate and the prefill rings without arrival flags that
- *     holds for a hidden V row too; the decode calls and the walk behind arrival
- *     flags multiply a hidden V by zero and need it finite.
+ *     cp_attn_partial_accumulate, cp_tree_attn and the prefill rings without arrival
+ *     flags that holds for a hidden V row too; the decode calls and the walk behind
+ *     arrival flags multiply a hidden V by zero and need it finite.
  */
 #ifndef CP_ATTN_H
 #define CP_ATTN_H
@@ -554,7 +554,8 @@ int cp_tree_mask(int32_t batch, const int32_t* cu_seqlens, const int32_t* parent
  *   workspace       cp_workspace_bytes(shape, CP_WS_TREE) bytes, 256-byte aligned
  *
  * bf16 and fp32, head_dim 64 and 128, any group of query heads. What a node does not see does not
- * reach it, NaN and infinity in hidden K and V rows included. Scores, statistics and accumulators
+ * reach it, NaN and infinity in hidden K and V rows included; an infinity in a V row that it sees is the
+ * result's (both signs: NaN), at several times the call's time. Scores, statistics and accumulators
  * are fp32; with bf16 inputs the probabilities are rounded to bf16 with head_dim 128 and a bf16 out only, else
  * they keep 24 bits. Two launches. Boundaries and counts on the device that contradict the shape
  * are cut to it: nothing outside the tensors is read or written.

@@ -96,8 +96,9 @@ __device__ __forceinline__ uint32_t div64(uint64_t a, uint32_t b) {   // quotien
 // It is cut into equal shares wherever they end, or, where there are few spans, so that no share
 // has tiles of two: a span takes as many workgroups as it needs at `share` tiles each. A workgroup with a second
 // piece (its Q, first tiles and result anew) is done as late as one with kPiece tiles more. us, anywhere and at spans'
-// ends: 61 nodes of 16 heads over 131072 keys 99.8 and 90.3, 16 sequences of 2048 to 8192 keys 70.9 and 66.4, 64 of 500 to
-// 4000 64.1 and 56.1, 8 of 900 to 6000 with head_dim 64 38.4 and 33.7, 32 of 1000 to 8000 with two nodes 34.2 and 29.2.
+// ends: 61 nodes of 16 heads over 131072 keys 98.9 and 88.7, 16 sequences of 2048 to 8192 keys 63.0 and 58.7, 64 of 500 to
+// 4000 with 16 nodes 59.8 and 52.9, 8 of 900 to 6000 with head_dim 64 and 30 to 100 nodes 40.0 and 35.0 (with 64 nodes each
+// 29.8 and 31.8), 32 of 1000 to 8000 with two nodes 28.2 and 25.3.
 template <int RM, int SPT>
 struct TreeLine {
   static constexpr int kPiece = SPT == 2 ? 8 : 4;
@@ -121,7 +122,7 @@ struct TreeLine {
     const int rows = mine.n * p.group;               // (in 31 bits: the host checks)
     mine.spans = (rows + RM - 1) / RM;
     // (blocks of the same height: the longest share decides. us, full blocks and a rest against equal ones: 272 rows on
-    // 8192 keys 26.0 and 23.7, on 8 times 4096 of 8 KV heads 103 and 90, 384 rows 107.5 and 98.2, 640 150 and 153)
+    // 8192 keys 26.0 and 24.2, on 8 times 4096 of 8 KV heads 100 and 84, 384 rows 105 and 98, 640 152 and 151)
     const uint32_t groups = (uint32_t)(rows + 31) / 32, spans = (uint32_t)max(mine.spans, 1);
     mine.rm = RM == 32 ? 32 : (int)((groups + spans - 1) / spans) * 32;
     if (b0 + (int)(threadIdx.x & 63) >= p.batch) mine.spans = 0;
@@ -331,7 +332,9 @@ __device__ __forceinline__ uint32_t ones_of(uint32_t bits, int i) {
 // one that sees an infinity has it as its result, whatever the weight (which may have become 0, and whose second and third
 // term may be negative: a NaN again). What the plain product leaves in such a row is the right infinity or a NaN, never
 // a finite number or the wrong sign. So nothing looks for such values on the way; where a result holds a NaN, the piece is
-// gone through a second time, with the values that are not finite set apart from the others in every sub-tile.
+// gone through a second time, with the values that are not finite set apart from the others in every sub-tile. (Where
+// every piece needs that, 16 trees over 2048 to 8192 keys with an fp32 result take 360 us instead of 92, 8 over 900 to
+// 6000 with head_dim 64 102 instead of 36; looking for such values in every masked sub-tile cost the others 1 to 7 us.)
 // NaN if the blocks hold one (or maybe an infinity: then the second pass is in vain).
 template <int N>
 __device__ __forceinline__ float nan_of(const floatx16_t (&o)[N]) {
@@ -362,8 +365,8 @@ constexpr int few_smem() {
 }
 
 // Bound by latencies: the chain {sequence boundaries} -> K, V, Q -> products -> join in LDS -> parts, and the
-// second launch; 8 nodes of 16 heads over 430 keys take 9 us here and 4 in the join, 32 sequences of 4096 keys at
-// 32 rows each 28.5 us (67 MB, 2.4 TB/s).
+// second launch; 8 nodes of 16 heads over 430 keys take 8 us here and 4 in the join, 32 sequences of 4096 keys at
+// 32 rows each 26.0 us (67 MB, 2.6 TB/s).
 // TI: K, V and Q. TO: O. P goes into the second product as TERMS bf16 terms (bf16 inputs): one at head_dim 128
 // where O is rounded to bf16 itself, three (24 bits) at head_dim 64, where cp_attn_partial keeps them too, and where O
 // stays fp32.
@@ -709,13 +712,15 @@ __global__ __launch_bounds__(FEW_WAVES * 64, sizeof(TI) * D == 512 ? 1 : 2) void
 // score exceeds it by 8 in powers of two (O and the sum are rescaled then): it cancels in O / l, and what is
 // rounded has the same relative error at any scale.
 // A tile goes straight into one of four LDS buffers: the tile before (its values), the current one, the next
-// and the one being filled; one barrier a tile. (Through registers, with fragments requested four products ahead
-// where now eight fit: 97 and 104 us for 61 nodes of 16 heads over 131072 keys, 88 and 95 for 16 sequences of 2048
-// to 8192 keys with three terms.)
-// Measured: 61 nodes of 16 heads over 131072 keys of one, 85 us, 770 TFLOP/s, of which 70 us are the loop (the matrix
-// pipe takes 2050 cycles of a tile's 3600), 9 the way to the first product and 4 the parts' way out. No one unit binds
-// the loop: without its LDS reads the call takes 0.92 of the time, without the exponentials 0.98, without the loads
-// 0.92; first requests by turns of the two wavefronts of a SIMD (their priority) change nothing.
+// and the one being filled; one barrier a tile. (When that was taken, against tiles through registers with fragments
+// requested four products ahead where now eight fit: 97 and 104 us for 61 nodes of 16 heads over 131072 keys, 88 and 95
+// for 16 sequences of 2048 to 8192 keys with three terms.)
+// Measured: 61 nodes of 16 heads over 131072 keys of one, 83.5 us, 784 TFLOP/s, of which 69 us are the loop (the matrix
+// pipe takes 2050 cycles of a tile's 3570), 12 the way to the first product and 4 the parts' way out. The matrix pipe is
+// busy for 43 % of the kernel and vector instructions are issued for 47 %: the two wavefronts of a SIMD come out of
+// a barrier together and mostly take turns at them, as do a wavefront's own (the prefill kernel's loop, whose LDS reads
+// are ordered by hand with counted waits, has the matrix pipe at 58 %). Without its LDS reads the call takes 0.92 of the
+// time, without the exponentials 0.98, without the loads 0.92; the wavefronts' priorities in turn change nothing.
 // ---------------------------------------------------------------------------
 constexpr int MANY_WAVES = 8;
 constexpr int MANY_ROWS = 32 * MANY_WAVES;
@@ -1100,7 +1105,7 @@ __global__ __launch_bounds__(MANY_WAVES * 64) void tree_many_kernel(const TreePa
       if (pc.t0 + 2 < pc.t1) request_tile(pc.t0 + 2, buf(pc.t0 + 2));
       if (!busy) {
         // none of the block's rows: the wavefront brings its part of the tiles and leaves the units to the others (64 rows
-        // of 32 sequences of 4096 keys 38.9 -> 29.7 us, 128 43.8 -> 32.2)
+        // of 32 sequences of 4096 keys 34.8 -> 29.4 us, 128 37.1 -> 31.5)
         for (int t = pc.t0; t < pc.t1; ++t) {
           landed_barrier();
           if (t + 3 < pc.t1) request_tile(t + 3, buf(t + 3));
@@ -1416,12 +1421,13 @@ TreePlan tree_plan(const cp_shape& s) {
   const int64_t group = s.n_q_heads / s.n_kv_heads;
   // 32-row blocks (of a sequence on average) times sub-tiles of all, weighed by head_dim: the form for many rows reads a
   // key once for 256 rows and has three times the matrix rate, the other starts and ends sooner, and one block of it
-  // is all the work there is up to 32 rows. us (few rows, many): head_dim 128, 16 heads on one: 8 sequences of 4096
-  // keys, 32 rows 17.5 and 19.5, 128 29.2 and 25.9, 256 39 and 32; 1 of 8192 keys, 256 rows 18.8 and 27.6, 640
-  // 26.4 and 29.9; 1 of 16384, 256 rows 28.2 and 30.5, 640 33.7 and 32.1; 32 sequences of 16 rows 25.0 and 25.2, of 64 38.3
-  // and 29.7; 32 heads on 8, 8 sequences of 32 rows 39 and 43, 32 of 32 133 and 117, of 64 179 and 121. Head_dim 64,
-  // 8 heads on two: 8 sequences of 128 rows 24.5 and 25.6, of 256 33.4 and 30.0; 32 sequences of 32 rows 24.5 and
-  // 35.0, of 64 33.0 and 34.6, of 128 56 and 39.
+  // is all the work there is up to 32 rows. us (few rows, many; * the one that the rule takes, where it is the slower):
+  // head_dim 128, 16 heads on one: 8 sequences of 4096 keys, 32 rows 17.5 and 18.4, 128 26.5 and 25.3, 256 36.5 and
+  // 30.8; 1 of 8192 keys, 256 rows 18.2 and 27.7, 640 24.1 and 29.0*; 1 of 16384, 256 rows 23.5 and 30.7*, 640 28.9
+  // and 30.9*; 32 sequences of 16 rows 24.4 and 25.4, of 64 36.2 and 29.8; 32 heads on 8, 8 sequences of 32 rows 42.0
+  // and 49.1*, 32 of 32 125 and 118, of 64 175 and 122. Head_dim 64, 8 heads on two: 8 sequences of 128 rows 25.7 and
+  // 26.8, of 256 36.1 and 32.7; 32 sequences of 32 rows 25.4 and 41.1, of 64 35.0 and 40.4*, of 128 56.8 and 44.9.
+  // (total_kv are the slots that there are, used or not, and the rows of a sequence are the batch's average.)
   const int64_t blocks = (s.total_q * group / s.batch + 31) / 32;
   const int64_t subs = ((s.total_kv + s.total_q) / SUB + s.batch) * s.n_kv_heads;
   const int64_t limit = (blocks > 1 ? kFewBlocks : kFewOneBlock) / (s.head_dim * s.head_dim);
@@ -1432,8 +1438,8 @@ TreePlan tree_plan(const cp_shape& s) {
   const int64_t spans = s.total_q * group / pl.rm + s.batch;
   const int64_t tiles = (s.total_kv + s.total_q) / (SUB * pl.spt) + 2 * (int64_t)s.batch;
   // (two workgroups of the form for few rows share a CU, which pays from a few tiles each. us for 256 and 512: 1 sequence
-  // of 8192 keys, 256 rows 18.8 and 23.8, 640 rows 28.2 and 26.4; 8 of 1024, 128 rows 18.0 and 20.6, 8 of 4096, 256
-  // rows 45 and 39; 32 heads on 8, 2048 keys, 64 rows 17.1 and 19.1)
+  // of 8192 keys, 256 rows 18.2 and 20.2, 640 rows 24.2 and 23.7; 8 of 1024, 128 rows 17.7 and 18.9, 8 of 4096, 256
+  // rows 39.2 and 36.5; 32 heads on 8, 2048 keys, 64 rows 17.5 and 18.0)
   const int64_t most = pl.many || blocks * subs / FEW_WAVES <= kFewTiles ? 256 : 512;
   const int64_t any = spans > most || tiles > most ? most : spans * tiles * s.n_kv_heads;
   while ((1 << pl.log2_wg) < any && (1 << pl.log2_wg) < most) ++pl.log2_wg;
