@@ -54,6 +54,16 @@ __device__ __forceinline__ int touch_arguments() {
   return x;
 }
 
+// Workgroups of one dimension, as a grid that can be launched: a dimension takes fewer than 2^32 threads (of
+// more, what passes 32 bits is lost without an error), so more than 2^22 workgroups go on in the second one. Those behind the last are the kernel's to end.
+inline dim3 wide_grid(int64_t blocks) {
+  constexpr int64_t row = 1 << 22;   // (of up to 1023 threads)
+  return blocks <= row ? dim3((unsigned)blocks) : dim3((unsigned)row, (unsigned)((blocks + row - 1) / row));
+}
+__device__ __forceinline__ int64_t wide_block() {
+  return (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+}
+
 // ---- checks of arguments, workspaces ----
 
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }

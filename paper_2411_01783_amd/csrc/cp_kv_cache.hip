@@ -61,7 +61,7 @@ __device__ __forceinline__ void commit_counts(const AppendParams& p) {
 
 template <bool TICKET>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendParams p) {
-  const int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+  const int64_t t = wide_block() * blockDim.x + threadIdx.x;
   const int64_t i = t / p.chunks_per_token;
   if (i < p.n_new) {
     const int c = (int)(t - i * p.chunks_per_token);
@@ -173,7 +173,7 @@ int cp_kv_append(const cp_shape* shape, const void* k_new, const void* v_new,
     hipLaunchKernelGGL(cp::kv_append_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, st, p);
     return hipGetLastError() == hipSuccess ? CP_OK : CP_ERR_LAUNCH;
   }
-  hipLaunchKernelGGL(cp::kv_append_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(cp::kv_append_kernel<false>, cp::wide_grid(blocks), dim3(256), 0, st, p);
   if (hipGetLastError() != hipSuccess) return CP_ERR_LAUNCH;
   hipLaunchKernelGGL(cp::kv_append_commit_kernel, dim3(1), dim3(256), 0, st, p);
   return hipGetLastError() == hipSuccess ? CP_OK : CP_ERR_LAUNCH;

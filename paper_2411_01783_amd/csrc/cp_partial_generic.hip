@@ -33,7 +33,7 @@ __global__ __launch_bounds__(kWaves * 64) void partial_generic_kernel(
   constexpr int DPL = D / 64;  // output dims per lane
   __shared__ float q_lds[kWaves][D];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * kWaves + wave;  // (token, head)
+  const int64_t row = wide_block() * kWaves + wave;  // (token, head)
   if (row >= total_q * n_q_heads) return;
   const int64_t tok = row / n_q_heads;
   const int h = (int)(row % n_q_heads);
@@ -99,10 +99,9 @@ int launch_t(const cp_shape& s, float scale, const void* q, const void* k, const
   if (rows == 0) return CP_OK;
   const int64_t blocks = (rows + kWaves - 1) / kWaves;
   if (blocks > 0x7fffffffLL) return CP_ERR_SHAPE;
-  hipLaunchKernelGGL((partial_generic_kernel<T, TO, D>), dim3((unsigned)blocks),
-                     dim3(kWaves * 64), 0, stream, (const T*)q, (const T*)k, (const T*)v, q_pos,
-                     kv_pos, cu_q, cu_kv, s.batch, s.total_q, s.total_kv, s.n_q_heads,
-                     s.n_kv_heads, scale, (TO*)out, lse);
+  hipLaunchKernelGGL((partial_generic_kernel<T, TO, D>), wide_grid(blocks), dim3(kWaves * 64), 0, stream,
+                     (const T*)q, (const T*)k, (const T*)v, q_pos, kv_pos, cu_q, cu_kv, s.batch,
+                     s.total_q, s.total_kv, s.n_q_heads, s.n_kv_heads, scale, (TO*)out, lse);
   return check_launch();
 }
 

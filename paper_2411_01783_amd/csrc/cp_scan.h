@@ -13,16 +13,6 @@ __device__ __forceinline__ int64_t clamp64(int64_t x, int64_t lo, int64_t hi) {
 // is what a call does (at 2^20 sequences of one node it would be half a minute).
 constexpr int32_t kMaxWalkedBatch = 65535;
 
-// Workgroups of one dimension, as a grid that can be launched: a dimension takes fewer than 2^32 threads, so more
-// than 2^22 workgroups go on in the second one. Those behind the last are the kernel's to end.
-inline dim3 wide_grid(int64_t blocks) {
-  constexpr int64_t row = 1 << 22;   // (of up to 1023 threads)
-  return blocks <= row ? dim3((unsigned)blocks) : dim3((unsigned)row, (unsigned)((blocks + row - 1) / row));
-}
-__device__ __forceinline__ int64_t wide_block() {
-  return (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
-}
-
 // Inclusive prefix sums on the vector pipe (data-parallel moves between lanes; a __shfl is a round
 // trip through LDS): over 16 lanes, over the wavefront.
 template <int CTRL, int ROWS>
